@@ -24,6 +24,8 @@
  * or with per-row selection into tile bitmaps:
  *   ugbs_select_rows  (Q, meta, trigger)     -> bitmap
  *   ugbs_attend_bitmap(Q, K, V, bitmap)      -> O
+ * and, for the tokens after the prompt, a paged cache in 8 bits:
+ *   ugbs_cache_plan, ugbs_cache_store, ugbs_cache_attend, ugbs_cache_load
  * No call synchronises the device; none allocates device memory.
  *
  * Diagnostics (Appendix D: sigma as a best-arm identification index), off
@@ -69,18 +71,21 @@ extern "C" {
 #define UGBS_API
 #endif
 
-#define UGBS_ABI_VERSION 10
+#define UGBS_ABI_VERSION 11
 #define UGBS_BLOCK 64          /* BLOCK_M = BLOCK_N = 64 tokens (Section 3.1, 3.2) */
 #define UGBS_MAX_BLOCKS 4096   /* N_B <= 4096, i.e. N <= 262144 */
 #define UGBS_MAX_BLOCKS_ROWS 2048 /* ugbs_select_rows, ugbs_bai_tiles, ugbs_bai_heads: N_B <= 2048 */
 #define UGBS_MAX_KV_WIDTH 4096 /* kv_width accepted by ugbs_attend; rho * k_budget <= 4096 */
 #define UGBS_MAX_RHO 8         /* expansion factor rho in 1..8 */
+#define UGBS_MAX_REQUESTS 4096 /* requests of a batch over the cache */
+#define UGBS_MAX_PAGES (1 << 24) /* pages of a cache (2^30 tokens) */
+#define UGBS_CACHE_RELEASE (-1) /* ugbs_cache_plan: the request gives its pages back */
 #define UGBS_ROUTE_SCRATCH_BYTES (1u << 20) /* device scratch of ugbs_route_noalloc, per GPU */
 
 typedef enum {
   UGBS_OK = 0,
   UGBS_ERR_NULL = 1,      /* a required pointer is NULL */
-  UGBS_ERR_SHAPE = 2,     /* batch/heads/seq_len/head_dim/block/kv_width invalid */
+  UGBS_ERR_SHAPE = 2,     /* batch/heads/seq_len/head_dim/block/kv_width/n_pages/max_pages/rows/width invalid */
   UGBS_ERR_BUDGET = 3,    /* k_budget < 3, rho outside [1, 8], or rho k_budget > 4096 */
   UGBS_ERR_Q = 4,         /* q outside [0, 1] or NaN */
   UGBS_ERR_BACKBONE = 5,  /* backbone not one of ugbs_backbone */
@@ -88,7 +93,9 @@ typedef enum {
   UGBS_ERR_WORKSPACE = 7, /* workspace NULL or smaller than ugbs_workspace_bytes */
   UGBS_ERR_HIP = 8,       /* a HIP launch failed */
   UGBS_ERR_SCALE = 9,     /* softmax_scale negative, NaN or infinite */
-  UGBS_ERR_SCRATCH = 10   /* the problem needs more than the static scratch of ugbs_route_noalloc */
+  UGBS_ERR_SCRATCH = 10,  /* the problem needs more than the static scratch of ugbs_route_noalloc */
+  UGBS_ERR_DTYPE = 11,    /* dtype not one of ugbs_cache_type */
+  UGBS_ERR_ALIAS = 12     /* an output of ugbs_cache_plan is one of its other arrays */
 } ugbs_status;
 
 /* Block-scoring backbone (Section 3.1).
@@ -411,6 +418,125 @@ UGBS_API int ugbs_attend_bitmap(const ugbs_problem* p, const void* Q, const void
  * It holds the route's sections (B T fp32 + B fp32 + B T bytes, each
  * 256-byte aligned), then B H (T-1)(T-2)/2 fp32 packed candidate scores. */
 UGBS_API size_t ugbs_workspace_bytes(const ugbs_problem* p);
+
+/* ---- The cache: keys and values of answered tokens in 8 bits ------------------
+ * After a prefill, the prompt's K and V are kept for the tokens that follow.  A
+ * cache is two device arrays owned by the caller, shared by all requests of a
+ * layer:
+ *   cache  : [n_pages, H_kv, 2, 64 d] bytes, 16-byte aligned: per page of 64
+ *            tokens and kv head the keys, then the values;
+ *   scales : [n_pages, H_kv, 2] fp32, 8-byte aligned: their scales.
+ * A byte stands for its number (e4m3: 4 exponent bits, bias 7, 3 fraction
+ * bits, largest 448, no infinities; or a signed integer, -127..127) times the
+ * scale.  Token t = 0..63 of a page, channel c:
+ *   keys   at [t / 16][c / 64][c % 64 / 16][t % 16][c % 16],
+ *   values at [t / 32][c / 32][t % 16 / 4][c % 16][c % 32 / 16][t % 32 / 16][t % 4]
+ * (the order in which the attention's matrix instructions take them).  What a
+ * page holds behind its request's last token is never used.
+ * A request's pages are listed in its row of
+ *   table  : [B, max_pages] int32: position j of request b lies in page
+ *            table[b, j / 64] at token j % 64.  Requests may list the same page
+ *            (a common prefix) as long as only reads reach it.  An entry outside
+ *            [0, n_pages) is no page: what would lie there is left out (its keys
+ *            are not attended, nothing is stored, loads give 0).
+ * One step of a batch, per layer but for the first call:
+ *   ugbs_cache_plan   (lengths)             -> table, slots, kv_lens, q_lens
+ *   ugbs_cache_store  (K, V, slots)         -> cache, scales
+ *   ugbs_cache_attend (Q, cache, ...)       -> O
+ * and ugbs_cache_load gives cached tokens back as bf16 K and V (exactly), for
+ * the prefill entry points above.  Lengths stay on the device, so a step can be
+ * captured in a HIP graph and replayed as lengths grow. */
+typedef enum { UGBS_E4M3 = 0, UGBS_INT8 = 1 } ugbs_cache_type;
+
+typedef struct ugbs_cache {
+  int32_t batch;        /* B requests, 1..UGBS_MAX_REQUESTS */
+  int32_t n_heads;      /* H >= 1, a multiple of n_kv_heads */
+  int32_t n_kv_heads;   /* H_kv >= 1 */
+  int32_t head_dim;     /* d: 64, 128 or 256 */
+  int32_t n_pages;      /* pages of the cache, 1..UGBS_MAX_PAGES */
+  int32_t max_pages;    /* entries of a table row, 1..UGBS_MAX_BLOCKS */
+  int32_t rows;         /* rows of Q, K, V, O and slots: new tokens of a request, 1..64 max_pages */
+  int32_t dtype;        /* ugbs_cache_type */
+  float softmax_scale;  /* attention logit scale; 0 means 1/sqrt(head_dim) */
+} ugbs_cache;
+
+/* Pages, slots and lengths of a step (one launch, integers only).
+ *   ctx_lens   : [B] int32, cached tokens of every request.
+ *   new_lens   : [B] int32, tokens to add, 0..rows; UGBS_CACHE_RELEASE gives the
+ *                request's pages back.
+ *   free_pages : [n_pages] int32, a stack of free page numbers, bottom first.
+ *   free_count : [1] int32, its height (taken as 0..n_pages).
+ *   table      : [B, max_pages] int32, read and extended in place.
+ *   kv_lens    : [B] int32 out: tokens of the request after the step.
+ *   q_lens     : [B] int32 out: tokens added.
+ *   slots      : [B, rows] int32 out: for each added token 64 page + token in
+ *                the page, -1 for the rows behind them (and where the table's entry
+ *                is no page).
+ *   free_left  : [1] int32 out: the stack's height after the step.
+ * In this order: the ceil(ctx / 64) pages of every released request are pushed,
+ * request by request and page by page (what passes n_pages is dropped); its
+ * kv_len and q_len are 0 and its table row stays as it is.  Then the requests take
+ * the ceil((ctx + new) / 64) - ceil(ctx / 64) pages they need from the top of the
+ * stack, in order; a request that needs pages is granted them when its need and
+ * those of all requests before it fit, else it adds nothing (q_len 0, kv_len ctx).
+ * The same holds for a request whose ctx, new or ctx + new does not fit (ctx
+ * outside 0..64 max_pages, which is taken as the nearest of these, new outside
+ * 0..rows, the sum above 64 max_pages): it needs no pages.
+ * All arrays are 4-byte aligned.  No output but table may overlap an input
+ * (UGBS_ERR_ALIAS where one begins at the same address). */
+UGBS_API int ugbs_cache_plan(const ugbs_cache* c, const int32_t* ctx_lens, const int32_t* new_lens,
+                             int32_t* free_pages, const int32_t* free_count, int32_t* table,
+                             int32_t* kv_lens, int32_t* q_lens, int32_t* slots, int32_t* free_left,
+                             void* stream);
+
+/* New tokens into the cache.
+ *   K, V  : [B, H_kv, rows, d] bf16, 16-byte aligned.
+ *   slots : [B, rows] int32 from ugbs_cache_plan: the rows of a request with a
+ *           slot come first and follow each other (slot i + 1 is the next token
+ *           of the page, or token 0 of another page).  A row whose slot breaks
+ *           this, or lies in no page, is not stored; where it would be the first
+ *           one in its page, the page's others aren't either.  Rows without a slot
+ *           are not read.  No two requests may add to the same page.
+ *   The scale of a page (per kv head, for keys and for values) is the smallest
+ *   power of two s >= 2^-100 with max |x| <= M s over the tokens it was given, M =
+ *   448 (e4m3) or 127.  Bytes are x / s, rounded once to nearest, ties to even.
+ *   A call whose first token of a page is token 0 starts the page anew; one that
+ *   goes on behind tokens 0..t-1 keeps their scale or raises it, and then rounds
+ *   their bytes times s_old / s_new again (exact for e4m3 but for its subnormals). */
+UGBS_API int ugbs_cache_store(const ugbs_cache* c, const void* K, const void* V, const int32_t* slots,
+                              void* cache, float* scales, void* stream);
+
+/* Cached tokens back as bf16 (exact: a byte's number has at most 7 significant
+ * bits and the scale is a power of two).
+ *   start : [B] int32, the first position read (taken as 0..64 max_pages).
+ *   count : [B] int32, positions read (taken as 0..width).
+ *   width : rows of K and V, 1..64 max_pages.
+ *   K, V  : [B, H_kv, width, d] bf16, 16-byte aligned: row i < count[b] gets
+ *           position start[b] + i; the other rows are left as they are.  A
+ *           position in no page gives 0. */
+UGBS_API int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float* scales, const int32_t* table,
+                             const int32_t* start, const int32_t* count, int32_t width, void* K, void* V,
+                             void* stream);
+
+/* Causal attention of the newest tokens of every request over its cache.
+ *   Row i < q_lens[b] of request b sits at position p_i = kv_lens[b] - q_lens[b] +
+ *   i and, for query head h and kv head h / (H / H_kv),
+ *   O_i = sum_{j <= p_i} softmax_j(scale * q_i . k_j) v_j with the cached k, v:
+ *   bf16 products, fp32 accumulation and softmax, probabilities rounded to bf16
+ *   for the second product.  A row that sees no key (p_i < 0, or no page) gives 0.
+ *   Q, O      : [B, H, rows, d] bf16, 16-byte aligned.  Rows q_lens[b] and up are
+ *               neither read nor written.
+ *   kv_lens   : [B] int32 (taken as 0..64 max_pages).
+ *   q_lens    : [B] int32 (taken as 0..rows).
+ *   workspace : device memory of at least ugbs_cache_workspace_bytes(c) bytes,
+ *               256-byte aligned, contents ignored (may be NULL when that is 0).
+ *               Two calls that overlap in time must not share it. */
+UGBS_API int ugbs_cache_attend(const ugbs_cache* c, const void* Q, const void* cache, const float* scales,
+                               const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, void* O,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of device workspace of ugbs_cache_attend (0 if c is invalid). */
+UGBS_API size_t ugbs_cache_workspace_bytes(const ugbs_cache* c);
 
 /* Static, human-readable text for a ugbs_status value. */
 UGBS_API const char* ugbs_status_string(int status);

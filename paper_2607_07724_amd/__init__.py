@@ -24,9 +24,13 @@ __all__ = [
     "ugbs_noise_scale", "ugbs_bai_tiles", "ugbs_bai_heads", "BAI_TILE_FIELDS", "BAI_HEAD_FIELDS",
     "bai_tile_records", "bai_head_records", "ugbs_route_noalloc", "ROUTE_SCRATCH_BYTES",
     "ugbs_quest_scores_valu",
+    "E4M3", "INT8", "CACHE_RELEASE", "Cache", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
+    "ugbs_cache_attend", "ugbs_cache_workspace_bytes", "CacheBuffers", "CacheStep", "prefill_cached", "cache_layer",
 ]
 
 KMEAN, QUEST = 0, 1
+E4M3, INT8 = 0, 1
+CACHE_RELEASE = -1
 BLOCK = 64
 MAX_BLOCKS = 4096
 MAX_BLOCKS_ROWS = 2048
@@ -87,6 +91,21 @@ class Problem(ctypes.Structure):
                 f"d={self.head_dim}, k={self.k_budget}, q={self.q}, backbone={self.backbone})")
 
 
+class Cache(ctypes.Structure):
+    """Mirror of ``ugbs_cache`` (include/ugbs.h)."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_heads", "n_kv_heads", "head_dim", "n_pages", "max_pages",
+                                              "rows", "dtype")] + [("softmax_scale", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, B, H, Hkv, d, n_pages, max_pages, rows=1, dtype=E4M3, scale=0.0):
+        return cls(B, H, Hkv, d, n_pages, max_pages, rows, dtype, float(scale))
+
+    def __repr__(self):
+        return (f"Cache(B={self.batch}, H={self.n_heads}, Hkv={self.n_kv_heads}, d={self.head_dim}, "
+                f"n_pages={self.n_pages}, max_pages={self.max_pages}, rows={self.rows}, "
+                f"dtype={'int8' if self.dtype == INT8 else 'e4m3'})")
+
+
 _lib = None
 
 
@@ -118,10 +137,18 @@ def lib():
         L.ugbs_bai_tiles.argtypes = [pp, P, P, P, ctypes.c_int32, P, P]
         L.ugbs_bai_heads.argtypes = [pp, P, P, ctypes.c_int32, P, P]
         L.ugbs_quest_scores_valu.argtypes = [pp, P, P, P, P]
+        pc = ctypes.POINTER(Cache)
+        L.ugbs_cache_plan.argtypes = [pc] + 10 * [P]
+        L.ugbs_cache_store.argtypes = [pc] + 6 * [P]
+        L.ugbs_cache_load.argtypes = [pc] + 5 * [P] + [ctypes.c_int32] + 3 * [P]
+        L.ugbs_cache_attend.argtypes = [pc] + 8 * [P] + [ctypes.c_size_t, P]
+        L.ugbs_cache_workspace_bytes.argtypes = [pc]
+        L.ugbs_cache_workspace_bytes.restype = ctypes.c_size_t
         for f in ("ugbs_block_meta", "ugbs_score_select", "ugbs_route", "ugbs_attend", "ugbs_abi_version",
                   "ugbs_attend_select", "ugbs_select_rows", "ugbs_attend_bitmap",
                   "ugbs_noise_scale", "ugbs_bai_tiles", "ugbs_bai_heads", "ugbs_route_noalloc",
-                  "ugbs_quest_scores_valu"):
+                  "ugbs_quest_scores_valu", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
+                  "ugbs_cache_attend"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -441,6 +468,86 @@ def ugbs_bai_heads(p: Problem, tiles, tau, n_samples, heads, stream=None):
                                                   _stream(stream)))
 
 
+# ---------------------------------------------------------------- cache
+
+def ugbs_cache_workspace_bytes(c: Cache) -> int:
+    return int(lib().ugbs_cache_workspace_bytes(ctypes.byref(c)))
+
+
+def _call(fn, dev, stream, c, *args):
+    """A cache entry point on `stream`, or on the current stream of the tensors' device."""
+    torch = _get_torch()
+    if dev.index == torch.cuda.current_device():
+        st = getattr(lib(), fn)(ctypes.byref(c), *args, _stream(stream))
+    else:
+        with torch.cuda.device(dev):
+            st = getattr(lib(), fn)(ctypes.byref(c), *args, _stream(stream))
+    _raise(fn, st)
+
+
+def _cache_arrays(c, cache, scales, dev):
+    torch = _get_torch()
+    if cache.dtype.itemsize != 1:
+        raise ValueError(f"cache: dtype {cache.dtype} is not of 8 bits")
+    return (_check("cache", cache, (c.n_pages, c.n_kv_heads, 2, BLOCK * c.head_dim), (cache.dtype,), dev),
+            _check("scales", scales, (c.n_pages, c.n_kv_heads, 2), (torch.float32,), dev))
+
+
+def ugbs_cache_plan(c: Cache, ctx_lens, new_lens, free_pages, free_count, table, kv_lens, q_lens, slots, free_left,
+                    stream=None):
+    """A step's pages, slots and lengths from the requests' lengths [B] int32 (new_lens CACHE_RELEASE: the
+    request's pages go back) and the stack free_pages [n_pages] of height free_count [1]: table
+    [B,max_pages] is extended, kv_lens, q_lens [B], slots [B,rows] and free_left [1] are written."""
+    i32 = (_get_torch().int32,)
+    dev, B = ctx_lens.device, c.batch
+    args = [_check(n, t, shape, i32, dev) for n, t, shape in (
+        ("ctx_lens", ctx_lens, (B,)), ("new_lens", new_lens, (B,)), ("free_pages", free_pages, (c.n_pages,)),
+        ("free_count", free_count, (1,)), ("table", table, (B, c.max_pages)), ("kv_lens", kv_lens, (B,)),
+        ("q_lens", q_lens, (B,)), ("slots", slots, (B, c.rows)), ("free_left", free_left, (1,)))]
+    _call("ugbs_cache_plan", dev, stream, c, *args)
+
+
+def ugbs_cache_store(c: Cache, K, V, slots, cache, scales, stream=None):
+    """K, V [B,Hkv,rows,d] bf16 into the pages of slots [B,rows] int32 (-1: no token): cache
+    [n_pages,Hkv,2,64 d] (any 8-bit dtype), scales [n_pages,Hkv,2] fp32."""
+    dev, shape = K.device, (c.batch, c.n_kv_heads, c.rows, c.head_dim)
+    k, v = _check("K", K, shape, _bf16()), _check("V", V, shape, _bf16(), dev)
+    sl = _check("slots", slots, (c.batch, c.rows), (_get_torch().int32,), dev)
+    _call("ugbs_cache_store", dev, stream, c, k, v, sl, *_cache_arrays(c, cache, scales, dev))
+
+
+def ugbs_cache_load(c: Cache, cache, scales, table, start, count, K, V, stream=None):
+    """Cached tokens as bf16: row i < count[b] of K, V [B,Hkv,width,d] gets position start[b] + i."""
+    if K.dim() != 4:
+        raise ValueError("K must be [B,Hkv,width,d]")
+    i32 = (_get_torch().int32,)
+    dev, width = K.device, int(K.shape[2])
+    shape = (c.batch, c.n_kv_heads, width, c.head_dim)
+    k, v = _check("K", K, shape, _bf16()), _check("V", V, shape, _bf16(), dev)
+    ca, sc = _cache_arrays(c, cache, scales, dev)
+    tb = _check("table", table, (c.batch, c.max_pages), i32, dev)
+    s0 = _check("start", start, (c.batch,), i32, dev)
+    n = _check("count", count, (c.batch,), i32, dev)
+    _call("ugbs_cache_load", dev, stream, c, ca, sc, tb, s0, n, width, k, v)
+
+
+def ugbs_cache_attend(c: Cache, Q, cache, scales, table, kv_lens, q_lens, O, workspace=None, stream=None):
+    """O [B,H,rows,d] = causal attention of the q_lens[b] newest tokens of every request over its kv_lens[b]
+    cached ones; rows behind q_lens[b] are left as they are."""
+    i32 = (_get_torch().int32,)
+    dev, shape = Q.device, (c.batch, c.n_heads, c.rows, c.head_dim)
+    q, o = _check("Q", Q, shape, _bf16()), _check("O", O, shape, _bf16(), dev)
+    ca, sc = _cache_arrays(c, cache, scales, dev)
+    tb = _check("table", table, (c.batch, c.max_pages), i32, dev)
+    kl = _check("kv_lens", kv_lens, (c.batch,), i32, dev)
+    ql = _check("q_lens", q_lens, (c.batch,), i32, dev)
+    ws, nbytes = None, 0
+    if workspace is not None:
+        ws = _check("workspace", workspace, workspace.shape, (workspace.dtype,), dev)
+        nbytes = workspace.numel() * workspace.element_size()
+    _call("ugbs_cache_attend", dev, stream, c, q, ca, sc, tb, kl, ql, o, ws, nbytes)
+
+
 # ---------------------------------------------------------------- convenience
 
 class Buffers:
@@ -478,6 +585,63 @@ def prefill_fused(p: Problem, Q, K, V, O, bufs: Buffers, stream=None):
     ugbs_score_select(p, Q, bufs.meta, None, bufs.sigma, stream=stream, workspace=bufs.workspace)
     ugbs_route(p, bufs.sigma, None, None, bufs.workspace, bufs.sigma_bar, bufs.tau, bufs.trigger, stream)
     ugbs_attend_select(p, Q, K, V, O, workspace=bufs.workspace, stream=stream)
+    return O
+
+
+class CacheBuffers:
+    """One layer's cache (allocated by torch)."""
+
+    def __init__(self, c: Cache, device="cuda"):
+        import torch
+        self.cache = torch.empty((c.n_pages, c.n_kv_heads, 2, BLOCK * c.head_dim), dtype=torch.uint8, device=device)
+        self.scales = torch.empty((c.n_pages, c.n_kv_heads, 2), dtype=torch.float32, device=device)
+
+
+class CacheStep:
+    """What the layers of a step share: table, free pages, lengths, slots and the attention's workspace
+    (allocated by torch).  At first all pages are free and all requests empty."""
+
+    def __init__(self, c: Cache, device="cuda"):
+        import torch
+        i32 = dict(dtype=torch.int32, device=device)
+        B = c.batch
+        self.table = torch.full((B, c.max_pages), -1, **i32)
+        self.free_pages = torch.arange(c.n_pages, **i32)
+        # the requests' lengths and the stack's height before a step, and after it
+        self._before = torch.zeros((B + 1,), **i32)
+        self._after = torch.zeros((B + 1,), **i32)
+        self._after[B] = c.n_pages
+        self.ctx_lens, self.free_count = self._before[:B], self._before[B:]
+        self.kv_lens, self.free_left = self._after[:B], self._after[B:]
+        self.q_lens = torch.zeros((B,), **i32)
+        self.slots = torch.full((B, c.rows), -1, **i32)
+        self.workspace = torch.empty((max(ugbs_cache_workspace_bytes(c), 256),), dtype=torch.uint8, device=device)
+
+    def plan(self, c: Cache, new_lens, stream=None):
+        """A step: every request goes on from its kv_lens with new_lens [B] int32 tokens.  Called once, before
+        the step's layers, on the current stream (or `stream`, as the layers' calls)."""
+        torch = _get_torch()
+        if stream is None:
+            torch.add(self._after, 0, out=self._before)
+        else:
+            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=self._after.device)):
+                torch.add(self._after, 0, out=self._before)
+        ugbs_cache_plan(c, self.ctx_lens, new_lens, self.free_pages, self.free_count, self.table, self.kv_lens,
+                        self.q_lens, self.slots, self.free_left, stream)
+
+
+def prefill_cached(p: Problem, c: Cache, Q, K, V, O, bufs: Buffers, cbufs: CacheBuffers, step: CacheStep, stream=None):
+    """prefill of prompts that begin with this step, their K and V kept in the cache (c.rows == p.seq_len;
+    step.plan comes first)."""
+    prefill(p, Q, K, V, O, bufs, stream)
+    ugbs_cache_store(c, K, V, step.slots, cbufs.cache, cbufs.scales, stream)
+    return O
+
+
+def cache_layer(c: Cache, Q, K, V, O, cbufs: CacheBuffers, step: CacheStep, stream=None):
+    """One layer of a step: the new tokens' K and V into the cache, then their attention over all of it."""
+    ugbs_cache_store(c, K, V, step.slots, cbufs.cache, cbufs.scales, stream)
+    ugbs_cache_attend(c, Q, cbufs.cache, cbufs.scales, step.table, step.kv_lens, step.q_lens, O, step.workspace, stream)
     return O
 
 

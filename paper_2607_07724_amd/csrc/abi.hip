@@ -69,7 +69,7 @@ const char* ugbs_status_string(int status) {
   switch (status) {
     case UGBS_OK: return "ok";
     case UGBS_ERR_NULL: return "a required pointer is NULL";
-    case UGBS_ERR_SHAPE: return "invalid shape (batch, heads, seq_len, head_dim, block or kv_width)";
+    case UGBS_ERR_SHAPE: return "invalid shape (batch, heads, seq_len, head_dim, block, kv_width, pages, rows or width)";
     case UGBS_ERR_BUDGET: return "k_budget < 3, rho outside [1, UGBS_MAX_RHO] or rho * k_budget > UGBS_MAX_KV_WIDTH";
     case UGBS_ERR_Q: return "q outside [0, 1]";
     case UGBS_ERR_BACKBONE: return "unknown backbone";
@@ -78,6 +78,8 @@ const char* ugbs_status_string(int status) {
     case UGBS_ERR_HIP: return "HIP launch failed";
     case UGBS_ERR_SCALE: return "softmax_scale negative or not finite";
     case UGBS_ERR_SCRATCH: return "problem exceeds the static scratch of ugbs_route_noalloc";
+    case UGBS_ERR_DTYPE: return "unknown cache type";
+    case UGBS_ERR_ALIAS: return "an output is one of the call's other arrays";
     default: return "unknown status";
   }
 }
