@@ -79,6 +79,7 @@ extern "C" {
 #define UGBS_MAX_RHO 8         /* expansion factor rho in 1..8 */
 #define UGBS_MAX_REQUESTS 4096 /* requests of a batch over the cache */
 #define UGBS_MAX_PAGES (1 << 24) /* pages of a cache (2^30 tokens) */
+#define UGBS_MAX_WIDTH (1 << 20) /* rows of a tensor that ugbs_cache_load fills */
 #define UGBS_CACHE_RELEASE (-1) /* ugbs_cache_plan: the request gives its pages back */
 #define UGBS_ROUTE_SCRATCH_BYTES (1u << 20) /* device scratch of ugbs_route_noalloc, per GPU */
 
@@ -510,10 +511,10 @@ UGBS_API int ugbs_cache_store(const ugbs_cache* c, const void* K, const void* V,
  * bits and the scale is a power of two).
  *   start : [B] int32, the first position read (taken as 0..64 max_pages).
  *   count : [B] int32, positions read (taken as 0..width).
- *   width : rows of K and V, 1..64 max_pages.
+ *   width : rows of K and V, 1..UGBS_MAX_WIDTH.
  *   K, V  : [B, H_kv, width, d] bf16, 16-byte aligned: row i < count[b] gets
  *           position start[b] + i; the other rows are left as they are.  A
- *           position in no page gives 0. */
+ *           position in no page, or behind the table, gives 0. */
 UGBS_API int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float* scales, const int32_t* table,
                              const int32_t* start, const int32_t* count, int32_t width, void* K, void* V,
                              void* stream);

@@ -89,7 +89,7 @@ int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float* scales,
   const int st = make_cache(c, &s);
   if (st) return st;
   if (!cache || !scales || !table || !start || !count || !K || !V) return UGBS_ERR_NULL;
-  if (width < 1 || width > s.max_pages * UGBS_BLOCK || !grid_fits((int64_t)s.B * s.Hkv, width)) return UGBS_ERR_SHAPE;
+  if (width < 1 || width > UGBS_MAX_WIDTH || !grid_fits((int64_t)s.B * s.Hkv, width)) return UGBS_ERR_SHAPE;
   if (!aligned(K, 16) || !aligned(V, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(table, 4) ||
       !aligned(start, 4) || !aligned(count, 4))
     return UGBS_ERR_ALIGN;
