@@ -32,7 +32,7 @@ ARCH = "gfx950"
 LLVM_BIN = "/opt/rocm/lib/llvm/bin"
 
 SOURCES = ["block_meta.hip", "score_select.hip", "route.hip", "attend.hip", "attend_keys.hip", "rowsel.hip", "bai.hip", "quest_valu.hip", "abi.hip",
-           "cache_plan.hip", "cache_store.hip", "cache_attend.hip", "cache_abi.hip"]
+           "cache_plan.hip", "cache_store.hip", "cache_attend.hip", "cache_tiles.hip", "cache_abi.hip"]
 PROBE_SOURCES = ["probe_peaks.hip"]
 
 CFLAGS = [
@@ -49,7 +49,8 @@ CFLAGS = [
 # attention kernel needs the accumulator registers for its budget.
 EXTRA_FLAGS = {"score_select.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "attend_keys.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "cache_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "cache_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "cache_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 PACKED_FP32 = re.compile(r"\bv_pk_(add|mul|fma)_f32\b")
 

@@ -1,0 +1,376 @@
+// What the kernels of the attention over the cache share: the parts of a call, the
+// pages of a part, the join.
+#pragma once
+#include "cache_internal.h"
+
+namespace ugbs {
+
+// Parts a call aims at, at most, and the pages of a part, at least: 128 KiB.
+constexpr int kTarget = 512;
+constexpr int min_pages(int d) { return 1024 / d; }
+// Every split tile has at least two parts, and parts of split tiles are at most twice W / X, X > W / target.
+constexpr int kSlots = 2 * kTarget;
+
+struct CacheAttendParams {
+  CacheShape s;
+  const uint16_t* Q;
+  const uint8_t* cache;
+  const float* scales;
+  const int32_t* table;
+  const int32_t* kv_lens;
+  const int32_t* q_lens;
+  uint16_t* O;
+  float* part_o;      // [slots][rows of a tile][D]: sums of p v, unnormalised
+  float2* part_ml;    // [slots][rows of a tile]: maximum (-inf: no key), sum of p
+  float scale_log2;
+  bool splits;        // parts are allowed
+  float per_part;     // 1 / parts aimed at (at most kTarget, a power of two)
+  int min_pages;
+};
+
+// Tiles of 64 (d 256: 32) rows, where rows are many (cache_tiles.hip).
+hipError_t launch_cache_tiles(const CacheAttendParams& P, hipStream_t stream);
+constexpr int tile_rows_many(int d) { return d == 256 ? 32 : 64; }
+
+namespace {
+
+constexpr float kNoMax = -3.402823466e38f;     // a row's maximum before its first key
+
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp(int x) {      // 0 where the lane has no source
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xf, false);
+}
+
+// Sum over lanes 0 .. l (shifts within 16 lanes, then the last lane of a row to the next rows).
+__device__ __forceinline__ int scan_add(int x) {
+  x += dpp<0x111, 0xf>(x);
+  x += dpp<0x112, 0xf>(x);
+  x += dpp<0x114, 0xf>(x);
+  x += dpp<0x118, 0xf>(x);
+  x += dpp<0x142, 0xa>(x);
+  x += dpp<0x143, 0xc>(x);
+  return x;
+}
+
+__device__ __forceinline__ float sum_groups(float x) {    // over lanes l, l ^ 16, l ^ 32, l ^ 48 (those that hold a row)
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ float sum_wave(float x) {      // over all lanes
+  auto add = [&](int y) { x += __uint_as_float((unsigned)y); };
+  add(dpp<0xb1, 0xf>((int)__float_as_uint(x)));           // lane ^ 1
+  add(dpp<0x4e, 0xf>((int)__float_as_uint(x)));           // lane ^ 2
+  add(dpp<0x141, 0xf>((int)__float_as_uint(x)));          // 7 - lane, within 8
+  add(dpp<0x140, 0xf>((int)__float_as_uint(x)));          // 15 - lane, within 16
+  return sum_groups(x);
+}
+
+// What a wave knows of a request: rows, tiles, pages.
+struct Lengths {
+  int q, kv, tiles, pages;
+};
+template <int ROWS>
+__device__ __forceinline__ Lengths lengths_of(const CacheAttendParams& P, int b) {
+  Lengths r;
+  r.q = min(max(P.q_lens[b], 0), P.s.rows);
+  r.kv = min(max(P.kv_lens[b], 0), P.s.max_pages * kBlock);
+  r.tiles = (r.q * P.s.G + ROWS - 1) / ROWS;
+  r.pages = (r.kv + kBlock - 1) / kBlock;
+  return r;
+}
+
+struct Part {
+  int b, kvh, tile, split, splits, slot, q, kv;   // slot: of the tile's first part
+};
+
+// Part number pos of the call (kJoinTiles: tile number pos among the split ones).
+// The parts of a request follow each other.  kParts: kv head, tile, part.  kGroups:
+// tiles that read the same pages (kv head, part) on one XCD, one after another, so
+// that its L2 serves all but the first: workgroup j runs on XCD j mod 8, so groups
+// are dealt out 8 at a time, those that are left over in a row.  Uniform over the wave.
+enum Order { kParts, kGroups, kJoinTiles };
+template <int ROWS, Order ORDER>
+__device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
+  const int lane = threadIdx.x & 63, B = P.s.B, Hkv = P.s.Hkv;
+  int per = UGBS_MAX_BLOCKS;
+  if (P.splits) {
+    // (fp32: every wave of both launches adds in the same order; + 1 covers the rounding, X being at most 4096)
+    float w = 0.f;
+    for (int b = lane; b < B; b += 64) {
+      const Lengths r = lengths_of<ROWS>(P, b);
+      w = __builtin_fmaf((float)r.tiles, (float)r.pages, w);
+    }
+    w = sum_wave(w) * (float)Hkv * P.per_part;
+    per = w < (float)UGBS_MAX_BLOCKS ? max((int)w + 1, P.min_pages) : UGBS_MAX_BLOCKS;
+    per = __builtin_amdgcn_readfirstlane(per);
+  }
+  int before = 0, slots = 0;
+  for (int c = 0; c < B; c += 64) {
+    Lengths r{0, 0, 0, 0};
+    int splits = 1;
+    if (c + lane < B) {
+      r = lengths_of<ROWS>(P, c + lane);
+      if (P.splits && r.pages > per) splits = (r.pages + per - 1) / per;
+    }
+    const int units = r.tiles * Hkv;
+    const int used = splits > 1 ? units * splits : 0;
+    const int mine = ORDER == kJoinTiles ? (splits > 1 ? units : 0) : units * splits;
+    const int upto = before + scan_add(mine), slots_upto = slots + scan_add(used);
+    const unsigned long long found = __ballot(pos >= upto - mine && pos < upto);
+    if (found) {
+      const int l = __builtin_ctzll(found);
+      out->b = c + l;
+      out->q = __builtin_amdgcn_readlane(r.q, l);
+      out->kv = __builtin_amdgcn_readlane(r.kv, l);
+      out->splits = __builtin_amdgcn_readlane(splits, l);
+      const int tiles = __builtin_amdgcn_readlane(r.tiles, l);
+      int at = pos - __builtin_amdgcn_readlane(upto - mine, l);
+      if (ORDER == kGroups) {
+        const int groups = Hkv * out->splits, dealt = groups / 8 * 8;
+        int group;
+        if (at < dealt * tiles) {
+          group = at / 8 / tiles * 8 + at % 8;
+          out->tile = at / 8 % tiles;
+        } else {
+          group = dealt + (at - dealt * tiles) / tiles;
+          out->tile = (at - dealt * tiles) % tiles;
+        }
+        out->split = group % out->splits;
+        out->kvh = group / out->splits;
+      } else {
+        out->split = 0;
+        if (ORDER == kParts) {
+          out->split = at % out->splits;
+          at /= out->splits;
+        }
+        out->tile = at % tiles;
+        out->kvh = at / tiles;
+      }
+      out->slot = __builtin_amdgcn_readlane(slots_upto - used, l) + (out->kvh * tiles + out->tile) * out->splits;
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+    slots = __builtin_amdgcn_readlane(slots_upto, 63);
+  }
+  return false;
+}
+
+// Pages that rows tile 16 .. + 15 see (the last row sees most).
+template <int ROWS>
+__device__ __forceinline__ int pages_seen(const CacheAttendParams& P, const Part& u) {
+  const int last = min((u.tile + 1) * ROWS, u.q * P.s.G) - 1;
+  const int end = u.kv - u.q + last / P.s.G + 1;          // keys the last row sees
+  return end <= 0 ? 0 : (end + kBlock - 1) / kBlock;
+}
+
+// 1 / l, for a row with maximum M: 0 where it saw no key, NaN where every score was -inf (as its softmax is).
+__device__ __forceinline__ float reciprocal(float M, float l) {
+  return M == -__builtin_huge_valf() ? 0.f : l != 0.f ? 1.0f / l : __builtin_nanf("");
+}
+
+// The pages of a part that one wave visits (p, p + step, ...), 64 at a time, one a
+// lane: its number and scales.  Entries that are no page are passed over.
+struct Pages {
+  const int32_t* row;
+  const float* scales;                      // of this kv head
+  int n_pages, stride, step, end;
+  int first;                                // page of lane 0
+  int id;
+  float2 scale;
+  unsigned long long left;                  // lanes whose page is still to visit
+
+  __device__ __forceinline__ void load() {
+    const int lane = threadIdx.x & 63;
+    for (;;) {
+      const int p = first + step * lane;
+      id = p < end ? row[p] : -1;
+      left = __ballot(id >= 0 && id < n_pages);
+      if (left || first + 64 * step >= end) break;
+      first += 64 * step;
+    }
+    scale = make_float2(0.f, 0.f);
+    if (left >> lane & 1) scale = *reinterpret_cast<const float2*>(scales + (size_t)id * stride);
+  }
+  // the next lane to visit, -1: none; the lanes may then be others
+  __device__ __forceinline__ int next() {
+    if (!left && first + 64 * step < end) {
+      first += 64 * step;
+      load();
+    }
+    if (!left) return -1;
+    const int l = __builtin_ctzll(left);
+    left &= left - 1;
+    return l;
+  }
+  __device__ __forceinline__ int page(int l) const { return __builtin_amdgcn_readlane(id, l); }
+  __device__ __forceinline__ int at(int l) const { return first + step * l; }
+  __device__ __forceinline__ float key_scale(int l) const {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale.x), l));
+  }
+  __device__ __forceinline__ float value_scale(int l) const {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(scale.y), l));
+  }
+};
+
+__device__ __forceinline__ Pages pages_of(const CacheAttendParams& P, const Part& u, int p0, int p1, int first, int step) {
+  Pages x;
+  x.row = P.table + (size_t)u.b * P.s.max_pages;
+  x.scales = P.scales + 2 * u.kvh;
+  x.n_pages = P.s.n_pages;
+  x.stride = 2 * P.s.Hkv;
+  x.step = step;
+  x.end = p1;
+  x.first = p0 + first;
+  x.load();
+  return x;
+}
+
+// Lane masks of the values' bytes of a half page from position key0 on: those
+// behind the last token may be anything and become 0 (a probability of 0 does not
+// make them harmless).
+__device__ __forceinline__ uint2 live_bytes(int kv, int key0) {
+  const int g = (threadIdx.x & 63) >> 4;
+  uint32_t keep[2];
+#pragma unroll
+  for (int kt = 0; kt < 2; ++kt) {
+    const int left = kv - (key0 + 16 * kt + 4 * g);
+    keep[kt] = left >= 4 ? ~0u : left <= 0 ? 0u : (1u << (8 * left)) - 1;
+  }
+  return make_uint2(keep[0], keep[1]);
+}
+
+// The waves' sums of a part, 16 rows at a time: O, or the part's slot.  seen: a
+// key of the row has been looked at.  s_o: [NW][16][D + 4] floats, s_ml: [NW][16 RT].
+template <int D, int RT, int NW>
+__device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Part& u, float* s_o, float2* s_ml,
+                                            const f32x4 (&acc)[RT][D / 16], const float (&m_run)[RT],
+                                            const float (&l_run)[RT], const bool (&seen)[RT]) {
+  constexpr int ROWS = 16 * RT, CG = D / 4, W = D + 4;   // 4 channels a thread
+  const CacheShape& s = P.s;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c16 = lane & 15;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float l = sum_groups(l_run[rt]);
+    if (g == 0) s_ml[w * ROWS + 16 * rt + c16] = make_float2(seen[rt] ? m_run[rt] : -__builtin_huge_valf(), l);
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    if (rt > 0) __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(s_o + (w * 16 + c16) * W + 16 * dt + 4 * g) = acc[rt][dt];
+    __syncthreads();
+    for (int k = tid; k < 16 * CG; k += 64 * NW) {
+      const int r16 = k / CG, c = 4 * (k % CG), rr = 16 * rt + r16;
+      const int at_row = u.tile * ROWS + rr;
+      if (at_row >= u.q * s.G) continue;
+      float M = -__builtin_huge_valf();
+#pragma unroll
+      for (int v = 0; v < NW; ++v) M = fmaxf(M, s_ml[v * ROWS + rr].x);
+      float l = 0.f;
+      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int v = 0; v < NW; ++v) {
+        const float2 ml = s_ml[v * ROWS + rr];
+        if (ml.x == -__builtin_huge_valf()) continue;     // this wave saw none of the row's keys
+        const float a = __builtin_amdgcn_exp2f(ml.x - M);
+        l += a * ml.y;
+        const f32x4 ov = *reinterpret_cast<const f32x4*>(s_o + (v * 16 + r16) * W + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += a * ov[e];
+      }
+      if (u.splits == 1) {
+        const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
+        const float inv = reciprocal(M, l);
+        *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + c) =
+            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+      } else {
+        const size_t slot = (size_t)u.slot + u.split;
+        *reinterpret_cast<f32x4*>(P.part_o + (slot * ROWS + rr) * D + c) = o;
+        if (c == 0) P.part_ml[slot * ROWS + rr] = make_float2(M, l);
+      }
+    }
+  }
+}
+
+// Joins the parts of one row: a workgroup per (split tile, row), D / 4 threads to
+// a part, the parts round the others.
+constexpr int kJoin = 256;
+template <int D, int ROWS>
+__global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) {
+  constexpr int CG = D / 4, GR = kJoin / CG;
+  __shared__ float s_w[kSlots];             // weights of the parts
+  __shared__ float2 s_ml[kJoin / 64];
+  __shared__ f32x4 s_o[GR][CG];
+  Part u;
+  if (!find_part<ROWS, kJoinTiles>(P, blockIdx.x, &u)) return;
+  const CacheShape& s = P.s;
+  const int tid = threadIdx.x, w = tid >> 6, rr = blockIdx.y, at_row = u.tile * ROWS + rr;
+  if (at_row >= u.q * s.G) return;
+  const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
+  float M = -__builtin_huge_valf();
+  for (int v = tid; v < u.splits; v += kJoin) {
+    const float m = ml[(size_t)v * ROWS].x;
+    s_w[v] = m;
+    M = fmaxf(M, m);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) s_ml[w].x = M;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kJoin / 64; ++v) M = fmaxf(M, s_ml[v].x);
+  float l = 0.f;
+  for (int v = tid; v < u.splits; v += kJoin) {
+    const float a = s_w[v] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(s_w[v] - M);
+    s_w[v] = a;
+    if (a != 0.f) l += a * ml[(size_t)v * ROWS].y;
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) l += __shfl_xor(l, o);
+  if ((tid & 63) == 0) s_ml[w].y = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int v = 0; v < kJoin / 64; ++v) l += s_ml[v].y;
+  const int gr = tid / CG, c = tid % CG;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
+#pragma unroll 4
+  for (int v = gr; v < u.splits; v += GR) {
+    const float a = s_w[v];
+    const f32x4 x = po[(size_t)v * (ROWS * CG)];
+    // (a part that saw none of the row's keys has written zeros)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += a * x[e];
+  }
+  s_o[gr][c] = o;
+  __syncthreads();
+  if (gr == 0) {
+#pragma unroll
+    for (int v = 1; v < GR; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += s_o[v][c][e];
+    const float inv = reciprocal(M, l);
+    const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
+    *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + 4 * c) =
+        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+  }
+}
+
+inline int64_t tiles_bound(const CacheShape& s, int rows_of_a_tile) {
+  return (int64_t)s.B * s.Hkv * (((int64_t)s.rows * s.G + rows_of_a_tile - 1) / rows_of_a_tile);
+}
+
+// Launches of the join, after the parts.
+template <int D, int ROWS>
+void launch_join(const CacheAttendParams& P, hipStream_t stream) {
+  const int64_t units = tiles_bound(P.s, ROWS), rows = (int64_t)P.s.rows * P.s.G;
+  const dim3 grid((unsigned)(units < kTarget ? units : kTarget), (unsigned)(rows < ROWS ? rows : ROWS));
+  cache_join_kernel<D, ROWS><<<grid, kJoin, 0, stream>>>(P);
+}
+
+}  // namespace
+}  // namespace ugbs

@@ -48,12 +48,13 @@ __host__ __device__ constexpr int value_at(int t, int c) {
 }
 
 // Four bytes of the cache as four bf16 (exact: e4m3 has 4 significant bits and
-// the integers 7).  The scale is applied elsewhere.
+// the integers 7).  e4m3: times a scale, a power of two, which the conversion takes
+// along; integers: the scale is applied elsewhere.
 template <int DT>
-__device__ __forceinline__ uint2 bytes_to_bf16(uint32_t w) {
+__device__ __forceinline__ uint2 bytes_to_bf16(uint32_t w, float scale) {
   if constexpr (DT == UGBS_E4M3) {
-    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false)),
-                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true)));
+    return make_uint2(__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false)),
+                      __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true)));
   } else {
     const float a = (float)(int8_t)w, b = (float)(int8_t)(w >> 8), c = (float)(int8_t)(w >> 16), d = (float)(int8_t)(w >> 24);
     return make_uint2(__builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u),
@@ -63,8 +64,8 @@ __device__ __forceinline__ uint2 bytes_to_bf16(uint32_t w) {
 
 // Eight bytes as the A operand of a matrix instruction.
 template <int DT>
-__device__ __forceinline__ bf16x8 operand(uint32_t lo, uint32_t hi) {
-  const uint2 a = bytes_to_bf16<DT>(lo), b = bytes_to_bf16<DT>(hi);
+__device__ __forceinline__ bf16x8 operand(uint32_t lo, uint32_t hi, float scale = 1.0f) {
+  const uint2 a = bytes_to_bf16<DT>(lo, scale), b = bytes_to_bf16<DT>(hi, scale);
   return as_bf16x8(make_uint4(a.x, a.y, b.x, b.y));
 }
 
