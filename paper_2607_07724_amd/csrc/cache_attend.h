@@ -296,12 +296,13 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
 }
 
 // Joins the parts of one row: a workgroup per (split tile, row), D / 4 threads to
-// a part, the parts round the others.
+// a part, the parts round the others.  The first kAhead parts of a thread are on
+// their way before the weights are known (latency is all there is here).
 constexpr int kJoin = 256;
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) {
-  constexpr int CG = D / 4, GR = kJoin / CG;
-  __shared__ float s_w[kSlots];             // weights of the parts
+  constexpr int CG = D / 4, GR = kJoin / CG, kAhead = 8;
+  __shared__ float2 s_part[kSlots];         // maximum, then weight; sum
   __shared__ float2 s_ml[kJoin / 64];
   __shared__ f32x4 s_o[GR][CG];
   Part u;
@@ -309,12 +310,19 @@ __global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) 
   const CacheShape& s = P.s;
   const int tid = threadIdx.x, w = tid >> 6, rr = blockIdx.y, at_row = u.tile * ROWS + rr;
   if (at_row >= u.q * s.G) return;
+  const int gr = tid / CG, c = tid % CG;
   const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
+  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
   float M = -__builtin_huge_valf();
   for (int v = tid; v < u.splits; v += kJoin) {
-    const float m = ml[(size_t)v * ROWS].x;
-    s_w[v] = m;
-    M = fmaxf(M, m);
+    s_part[v] = ml[(size_t)v * ROWS];
+    M = fmaxf(M, s_part[v].x);
+  }
+  f32x4 ahead[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k) {
+    const int v = gr + k * GR;
+    ahead[k] = po[(size_t)min(v, u.splits - 1) * (ROWS * CG)];
   }
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
@@ -324,28 +332,29 @@ __global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) 
   for (int v = 0; v < kJoin / 64; ++v) M = fmaxf(M, s_ml[v].x);
   float l = 0.f;
   for (int v = tid; v < u.splits; v += kJoin) {
-    const float a = s_w[v] == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(s_w[v] - M);
-    s_w[v] = a;
-    if (a != 0.f) l += a * ml[(size_t)v * ROWS].y;
+    const float2 x = s_part[v];
+    // a part that saw none of the row's keys weighs nothing
+    const float a = x.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(x.x - M);
+    s_part[v].x = a;
+    if (a != 0.f) l += a * x.y;
   }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) l += __shfl_xor(l, o);
+  l = sum_wave(l);
   if ((tid & 63) == 0) s_ml[w].y = l;
   __syncthreads();
   l = 0.f;
 #pragma unroll
   for (int v = 0; v < kJoin / 64; ++v) l += s_ml[v].y;
-  const int gr = tid / CG, c = tid % CG;
   f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
-#pragma unroll 4
-  for (int v = gr; v < u.splits; v += GR) {
-    const float a = s_w[v];
-    const f32x4 x = po[(size_t)v * (ROWS * CG)];
-    // (a part that saw none of the row's keys has written zeros)
+  auto add = [&](int v, const f32x4& x) {
+    const float a = s_part[v].x;
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += a * x[e];
-  }
+  };
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (gr + k * GR < u.splits) add(gr + k * GR, ahead[k]);
+#pragma unroll 4
+  for (int v = gr + kAhead * GR; v < u.splits; v += GR) add(v, po[(size_t)v * (ROWS * CG)]);
   s_o[gr][c] = o;
   __syncthreads();
   if (gr == 0) {

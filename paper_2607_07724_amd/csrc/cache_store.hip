@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(2 * D) cache_load_kernel(CacheShape s, const u
     vs = sc[1];
     const uint4* const src = reinterpret_cast<const uint4*>(cache + ((size_t)page * s.Hkv + kvh) * 2 * (kBlock * D));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(s_page)[e * 2 * D + tid] = src[e * 2 * D + tid];
+    for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(s_page)[e * 2 * D + tid] = load_once(src + e * 2 * D + tid);
   }
   __syncthreads();
   const int cg = tid % CG, tg = tid / CG, c0 = 8 * cg;

@@ -15,8 +15,21 @@
 namespace ugbs {
 namespace {
 
+// ONCE: the rows of a kv head are one tile, so a byte is read once and not kept in the caches.
+template <bool ONCE>
+__device__ __forceinline__ void dma16_cache(const uint8_t* base, uint32_t voff, uint32_t lds_byte_addr) {
+  if constexpr (ONCE) {
+    asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+                 :
+                 : "v"(voff), "s"(base), "s"(lds_byte_addr)
+                 : "memory");
+  } else {
+    dma16(reinterpret_cast<const uint16_t*>(base), voff, lds_byte_addr);
+  }
+}
+
 // One part: RT tiles of 16 rows against pages p0 .. p1 - 1.
-template <int D, int DT, int RT, int QR, int NW, int WPE>
+template <int D, int DT, int RT, int QR, int NW, int WPE, bool ONCE>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 cache_tiles_kernel(CacheAttendParams P) {
   constexpr int L = D / 32, E = D / 64;     // loads of a half page's keys (values); 64-channel steps
@@ -48,10 +61,10 @@ cache_tiles_kernel(CacheAttendParams P) {
   const uint32_t k_lds = __builtin_amdgcn_readfirstlane(lds_addr(tk)), v_lds = k_lds + kTile;
   const uint32_t off = 16 * lane;
   auto load_k = [&](int page, int j) {
-    dma16(reinterpret_cast<const uint16_t*>(cache + page * page_stride + j * 1024), off, k_lds + j * 1024);
+    dma16_cache<ONCE>(cache + page * page_stride + j * 1024, off, k_lds + j * 1024);
   };
   auto load_v = [&](int page, int j) {
-    dma16(reinterpret_cast<const uint16_t*>(cache + page * page_stride + kBlock * D + j * 1024), off, v_lds + j * 1024);
+    dma16_cache<ONCE>(cache + page * page_stride + kBlock * D + j * 1024, off, v_lds + j * 1024);
   };
 
   Pages pages = pages_of(P, u, p0, p1, w >> 1, NW / 2);
@@ -234,7 +247,9 @@ hipError_t tiles(const CacheAttendParams& P, hipStream_t stream) {
   constexpr int NW = 4, ROWS = 16 * RT;
   static_assert(ROWS == tile_rows_many(D), "rows of a tile");
   const int64_t units = tiles_bound(P.s, ROWS);
-  cache_tiles_kernel<D, DT, RT, QR, NW, WPE><<<(unsigned)(units + (P.splits ? kTarget : 0)), 64 * NW, 0, stream>>>(P);
+  const unsigned grid = (unsigned)(units + (P.splits ? kTarget : 0));
+  if ((int64_t)P.s.rows * P.s.G <= ROWS) cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true><<<grid, 64 * NW, 0, stream>>>(P);
+  else cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false><<<grid, 64 * NW, 0, stream>>>(P);
   if (P.splits) launch_join<D, ROWS>(P, stream);
   return hipGetLastError();
 }
