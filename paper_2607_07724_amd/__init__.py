@@ -172,13 +172,14 @@ def ugbs_workspace_bytes(p: Problem) -> int:
 # for as a raw handle, and a call's sizes are read from the problem once.
 
 _torch = None
-_BF16 = ()
+_BF16 = _I32 = _F32 = ()
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _BF16, _raw_stream
+    global _torch, _BF16, _I32, _F32, _raw_stream
     import torch
+    _I32, _F32 = (torch.int32,), (torch.float32,)
     _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _torch = torch
@@ -474,23 +475,37 @@ def ugbs_cache_workspace_bytes(c: Cache) -> int:
     return int(lib().ugbs_cache_workspace_bytes(ctypes.byref(c)))
 
 
-def _call(fn, dev, stream, c, *args):
+def _addr(name, t, shape, dtypes, index, dev):
+    """_check's answer, with fewer steps where nothing is wrong (a decode step makes these calls once a layer)."""
+    if t is None or t.shape != shape or t.dtype not in dtypes or t.get_device() != index or not t.is_contiguous():
+        return _check(name, t, shape, dtypes, dev)
+    return t.data_ptr()
+
+
+def _call(fn, index, stream, c, *args):
     """A cache entry point on `stream`, or on the current stream of the tensors' device."""
-    torch = _get_torch()
-    if dev.index == torch.cuda.current_device():
-        st = getattr(lib(), fn)(ctypes.byref(c), *args, _stream(stream))
+    torch = _torch
+    if index == torch.cuda.current_device():
+        st = getattr(_lib or lib(), fn)(ctypes.byref(c), *args, _raw_stream(index) if stream is None and _raw_stream
+                                        else _stream(stream))
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(index):
             st = getattr(lib(), fn)(ctypes.byref(c), *args, _stream(stream))
-    _raise(fn, st)
+    if st != 0:
+        _raise(fn, st)
 
 
-def _cache_arrays(c, cache, scales, dev):
-    torch = _get_torch()
+def _device_of(name, t):
+    if t is None or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    return t.get_device(), t.device
+
+
+def _cache_arrays(c, cache, scales, pages, Hkv, d, index, dev):
     if cache.dtype.itemsize != 1:
         raise ValueError(f"cache: dtype {cache.dtype} is not of 8 bits")
-    return (_check("cache", cache, (c.n_pages, c.n_kv_heads, 2, BLOCK * c.head_dim), (cache.dtype,), dev),
-            _check("scales", scales, (c.n_pages, c.n_kv_heads, 2), (torch.float32,), dev))
+    return (_addr("cache", cache, (pages, Hkv, 2, BLOCK * d), (cache.dtype,), index, dev),
+            _addr("scales", scales, (pages, Hkv, 2), _F32, index, dev))
 
 
 def ugbs_cache_plan(c: Cache, ctx_lens, new_lens, free_pages, free_count, table, kv_lens, q_lens, slots, free_left,
@@ -498,54 +513,58 @@ def ugbs_cache_plan(c: Cache, ctx_lens, new_lens, free_pages, free_count, table,
     """A step's pages, slots and lengths from the requests' lengths [B] int32 (new_lens CACHE_RELEASE: the
     request's pages go back) and the stack free_pages [n_pages] of height free_count [1]: table
     [B,max_pages] is extended, kv_lens, q_lens [B], slots [B,rows] and free_left [1] are written."""
-    i32 = (_get_torch().int32,)
-    dev, B = ctx_lens.device, c.batch
-    args = [_check(n, t, shape, i32, dev) for n, t, shape in (
-        ("ctx_lens", ctx_lens, (B,)), ("new_lens", new_lens, (B,)), ("free_pages", free_pages, (c.n_pages,)),
-        ("free_count", free_count, (1,)), ("table", table, (B, c.max_pages)), ("kv_lens", kv_lens, (B,)),
-        ("q_lens", q_lens, (B,)), ("slots", slots, (B, c.rows)), ("free_left", free_left, (1,)))]
-    _call("ugbs_cache_plan", dev, stream, c, *args)
+    _get_torch()
+    x, dev = _device_of("ctx_lens", ctx_lens)
+    i, one = _I32, (c.batch,)
+    _call("ugbs_cache_plan", x, stream, c,
+          _addr("ctx_lens", ctx_lens, one, i, x, dev), _addr("new_lens", new_lens, one, i, x, dev),
+          _addr("free_pages", free_pages, (c.n_pages,), i, x, dev), _addr("free_count", free_count, (1,), i, x, dev),
+          _addr("table", table, (c.batch, c.max_pages), i, x, dev), _addr("kv_lens", kv_lens, one, i, x, dev),
+          _addr("q_lens", q_lens, one, i, x, dev), _addr("slots", slots, (c.batch, c.rows), i, x, dev),
+          _addr("free_left", free_left, (1,), i, x, dev))
 
 
 def ugbs_cache_store(c: Cache, K, V, slots, cache, scales, stream=None):
     """K, V [B,Hkv,rows,d] bf16 into the pages of slots [B,rows] int32 (-1: no token): cache
     [n_pages,Hkv,2,64 d] (any 8-bit dtype), scales [n_pages,Hkv,2] fp32."""
-    dev, shape = K.device, (c.batch, c.n_kv_heads, c.rows, c.head_dim)
-    k, v = _check("K", K, shape, _bf16()), _check("V", V, shape, _bf16(), dev)
-    sl = _check("slots", slots, (c.batch, c.rows), (_get_torch().int32,), dev)
-    _call("ugbs_cache_store", dev, stream, c, k, v, sl, *_cache_arrays(c, cache, scales, dev))
+    _get_torch()
+    x, dev = _device_of("K", K)
+    B, Hkv, d, rows = c.batch, c.n_kv_heads, c.head_dim, c.rows
+    shape = (B, Hkv, rows, d)
+    _call("ugbs_cache_store", x, stream, c,
+          _addr("K", K, shape, _BF16, x, dev), _addr("V", V, shape, _BF16, x, dev),
+          _addr("slots", slots, (B, rows), _I32, x, dev), *_cache_arrays(c, cache, scales, c.n_pages, Hkv, d, x, dev))
 
 
 def ugbs_cache_load(c: Cache, cache, scales, table, start, count, K, V, stream=None):
     """Cached tokens as bf16: row i < count[b] of K, V [B,Hkv,width,d] gets position start[b] + i."""
+    _get_torch()
+    x, dev = _device_of("K", K)
     if K.dim() != 4:
         raise ValueError("K must be [B,Hkv,width,d]")
-    i32 = (_get_torch().int32,)
-    dev, width = K.device, int(K.shape[2])
-    shape = (c.batch, c.n_kv_heads, width, c.head_dim)
-    k, v = _check("K", K, shape, _bf16()), _check("V", V, shape, _bf16(), dev)
-    ca, sc = _cache_arrays(c, cache, scales, dev)
-    tb = _check("table", table, (c.batch, c.max_pages), i32, dev)
-    s0 = _check("start", start, (c.batch,), i32, dev)
-    n = _check("count", count, (c.batch,), i32, dev)
-    _call("ugbs_cache_load", dev, stream, c, ca, sc, tb, s0, n, width, k, v)
+    B, Hkv, d, width = c.batch, c.n_kv_heads, c.head_dim, int(K.shape[2])
+    shape = (B, Hkv, width, d)
+    _call("ugbs_cache_load", x, stream, c, *_cache_arrays(c, cache, scales, c.n_pages, Hkv, d, x, dev),
+          _addr("table", table, (B, c.max_pages), _I32, x, dev), _addr("start", start, (B,), _I32, x, dev),
+          _addr("count", count, (B,), _I32, x, dev), width,
+          _addr("K", K, shape, _BF16, x, dev), _addr("V", V, shape, _BF16, x, dev))
 
 
 def ugbs_cache_attend(c: Cache, Q, cache, scales, table, kv_lens, q_lens, O, workspace=None, stream=None):
     """O [B,H,rows,d] = causal attention of the q_lens[b] newest tokens of every request over its kv_lens[b]
     cached ones; rows behind q_lens[b] are left as they are."""
-    i32 = (_get_torch().int32,)
-    dev, shape = Q.device, (c.batch, c.n_heads, c.rows, c.head_dim)
-    q, o = _check("Q", Q, shape, _bf16()), _check("O", O, shape, _bf16(), dev)
-    ca, sc = _cache_arrays(c, cache, scales, dev)
-    tb = _check("table", table, (c.batch, c.max_pages), i32, dev)
-    kl = _check("kv_lens", kv_lens, (c.batch,), i32, dev)
-    ql = _check("q_lens", q_lens, (c.batch,), i32, dev)
+    _get_torch()
+    x, dev = _device_of("Q", Q)
+    B, d = c.batch, c.head_dim
+    shape, one = (B, c.n_heads, c.rows, d), (B,)
     ws, nbytes = None, 0
     if workspace is not None:
-        ws = _check("workspace", workspace, workspace.shape, (workspace.dtype,), dev)
-        nbytes = workspace.numel() * workspace.element_size()
-    _call("ugbs_cache_attend", dev, stream, c, q, ca, sc, tb, kl, ql, o, ws, nbytes)
+        ws = _addr("workspace", workspace, workspace.shape, (workspace.dtype,), x, dev)
+        nbytes = workspace.nbytes
+    _call("ugbs_cache_attend", x, stream, c, _addr("Q", Q, shape, _BF16, x, dev),
+          *_cache_arrays(c, cache, scales, c.n_pages, c.n_kv_heads, d, x, dev),
+          _addr("table", table, (B, c.max_pages), _I32, x, dev), _addr("kv_lens", kv_lens, one, _I32, x, dev),
+          _addr("q_lens", q_lens, one, _I32, x, dev), _addr("O", O, shape, _BF16, x, dev), ws, nbytes)
 
 
 # ---------------------------------------------------------------- convenience

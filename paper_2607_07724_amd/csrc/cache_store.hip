@@ -100,14 +100,18 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
   const int off = s0 % kBlock;
   const int i0 = max(0, j * kBlock - off);
   if (i0 >= s.rows) return;
+  const int i1 = min(s.rows, (j + 1) * kBlock - off), t0 = j == 0 ? off : 0;
+  // this thread's 4 tokens and 8 channels; the slots of its rows come with the first one's
+  const int cg = tid % CG, tg = tid / CG, c0 = 8 * cg;
+  int mine[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) mine[e] = slot[min(max(i0 + 4 * tg + e - t0, i0), i1 - 1)];
   const int first = slot[i0];               // the page's first new token
   if (first < 0) return;
-  const int page = first / kBlock, t0 = j == 0 ? off : 0;
+  const int page = first / kBlock;
   if (page >= s.n_pages || first % kBlock != t0) return;
-  const int i1 = min(s.rows, (j + 1) * kBlock - off);
-
-  // this thread's 4 tokens and 8 channels
-  const int cg = tid % CG, tg = tid / CG, c0 = 8 * cg;
+  float* const sc = scales + 2 * ((size_t)page * s.Hkv + kvh);
+  const float2 old = t0 > 0 ? *reinterpret_cast<const float2*>(sc) : make_float2(0.f, 0.f);
   uint4 k[4], v[4];
   uint32_t live = 0, ka = 0, va = 0;        // live: bit t of the thread's tokens that are new here
   const size_t base = ((size_t)b * s.Hkv + kvh) * s.rows;
@@ -116,7 +120,7 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
     const int t = 4 * tg + e, i = i0 + t - t0;
     k[e] = v[e] = make_uint4(0, 0, 0, 0);
     // a row whose slot is not the next one of the page is left out
-    if (i >= i0 && i < i1 && slot[i] == page * kBlock + t) {
+    if (i >= i0 && i < i1 && mine[e] == page * kBlock + t) {
       live |= 1u << e;
       k[e] = *reinterpret_cast<const uint4*>(K + (base + i) * D + c0);
       v[e] = *reinterpret_cast<const uint4*>(V + (base + i) * D + c0);
@@ -143,14 +147,12 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
     va = max(va, s_amax[x][1]);
   }
   float ks = scale_for<DT>(ka), vs = scale_for<DT>(va);
-  float* const sc = scales + 2 * ((size_t)page * s.Hkv + kvh);
   uint8_t* const kp = cache + ((size_t)page * s.Hkv + kvh) * 2 * (kBlock * D);
   uint8_t* const vp = kp + kBlock * D;
   if (t0 > 0) {
-    const float ks_old = sc[0], vs_old = sc[1];
-    ks = fmaxf(ks, ks_old);
-    vs = fmaxf(vs, vs_old);
-    const float kr = ks_old / ks, vr = vs_old / vs;
+    ks = fmaxf(ks, old.x);
+    vs = fmaxf(vs, old.y);
+    const float kr = old.x / ks, vr = old.y / vs;
     // tokens 0 .. t0 - 1 move to the larger scale
     if (kr < 1.0f) {
       for (int at = tid; at < kBlock * D / 16; at += 2 * D) {       // 16 channels of one token
@@ -214,10 +216,7 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
         }
     }
   }
-  if (tid == 0) {
-    sc[0] = ks;
-    sc[1] = vs;
-  }
+  if (tid == 0) *reinterpret_cast<float2*>(sc) = make_float2(ks, vs);
 }
 
 // Cached tokens as bf16.  One workgroup per (request, kv head, page of the
