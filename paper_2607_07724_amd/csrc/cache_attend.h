@@ -11,6 +11,16 @@ constexpr int min_pages(int d) { return 1024 / d; }
 // Every split tile has at least two parts, and parts of split tiles are at most twice W / X, X > W / target.
 constexpr int kSlots = 2 * kTarget;
 
+// Where the parts lie, of batches of more than kWaveBatch requests: formed once by
+// cache_schedule_kernel, in the workspace.  Up to kWaveBatch every wave forms it for itself
+// (4 lengths a lane), which is quicker than a launch.
+constexpr int kWaveBatch = 256;
+struct Schedule {
+  int4* request;      // [B]: parts before, parts of a tile, slots before, split tiles before
+  int32_t* part;      // [tiles + kTarget]: the request, -1 behind the last part
+  int32_t* join;      // [kTarget]: the same for the split tiles
+};
+
 struct CacheAttendParams {
   CacheShape s;
   const uint16_t* Q;
@@ -24,6 +34,7 @@ struct CacheAttendParams {
   float2* part_ml;    // [slots][rows of a tile]: maximum (-inf: no key), sum of p
   float scale_log2;
   bool splits;        // parts are allowed
+  Schedule schedule;  // of more than kWaveBatch requests
   float per_part;     // 1 / parts aimed at (at most kTarget, a power of two)
   int min_pages;
 };
@@ -35,22 +46,6 @@ constexpr int tile_rows_many(int d) { return d == 256 ? 32 : 64; }
 namespace {
 
 constexpr float kNoMax = -3.402823466e38f;     // a row's maximum before its first key
-
-template <int CTRL, int ROW_MASK>
-__device__ __forceinline__ int dpp(int x) {      // 0 where the lane has no source
-  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xf, false);
-}
-
-// Sum over lanes 0 .. l (shifts within 16 lanes, then the last lane of a row to the next rows).
-__device__ __forceinline__ int scan_add(int x) {
-  x += dpp<0x111, 0xf>(x);
-  x += dpp<0x112, 0xf>(x);
-  x += dpp<0x114, 0xf>(x);
-  x += dpp<0x118, 0xf>(x);
-  x += dpp<0x142, 0xa>(x);
-  x += dpp<0x143, 0xc>(x);
-  return x;
-}
 
 __device__ __forceinline__ float sum_groups(float x) {    // over lanes l, l ^ 16, l ^ 32, l ^ 48 (those that hold a row)
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -86,70 +81,90 @@ struct Part {
   int b, kvh, tile, split, splits, slot, q, kv;   // slot: of the tile's first part
 };
 
+// Pages per part, from the sum over the requests of tiles times pages (fp32, added in
+// the same order wherever it is formed; + 1 covers the rounding, X being at most 4096).
+__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work) {
+  if (!P.splits) return UGBS_MAX_BLOCKS;
+  const float x = work * (float)P.s.Hkv * P.per_part;
+  return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, P.min_pages) : UGBS_MAX_BLOCKS;
+}
+__device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.pages > per ? (r.pages + per - 1) / per : 1; }
+
 // Part number pos of the call (kJoinTiles: tile number pos among the split ones).
 // The parts of a request follow each other.  kParts: kv head, tile, part.  kGroups:
 // tiles that read the same pages (kv head, part) on one XCD, one after another, so
 // that its L2 serves all but the first: workgroup j runs on XCD j mod 8, so groups
 // are dealt out 8 at a time, those that are left over in a row.  Uniform over the wave.
 enum Order { kParts, kGroups, kJoinTiles };
+template <Order ORDER>
+__device__ __forceinline__ void locate(const CacheAttendParams& P, int at, int tiles, int slots_before, Part* out) {
+  out->split = 0;
+  if (ORDER == kGroups) {
+    const int groups = P.s.Hkv * out->splits, dealt = groups / 8 * 8;
+    int group;
+    if (at < dealt * tiles) {
+      group = at / 8 / tiles * 8 + at % 8;
+      out->tile = at / 8 % tiles;
+    } else {
+      group = dealt + (at - dealt * tiles) / tiles;
+      out->tile = (at - dealt * tiles) % tiles;
+    }
+    out->split = group % out->splits;
+    out->kvh = group / out->splits;
+  } else {
+    if (ORDER == kParts) {
+      out->split = at % out->splits;
+      at /= out->splits;
+    }
+    out->tile = at % tiles;
+    out->kvh = at / tiles;
+  }
+  out->slot = slots_before + (out->kvh * tiles + out->tile) * out->splits;
+}
+
 template <int ROWS, Order ORDER>
 __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
   const int lane = threadIdx.x & 63, B = P.s.B, Hkv = P.s.Hkv;
-  int per = UGBS_MAX_BLOCKS;
-  if (P.splits) {
-    // (fp32: every wave of both launches adds in the same order; + 1 covers the rounding, X being at most 4096)
-    float w = 0.f;
-    for (int b = lane; b < B; b += 64) {
-      const Lengths r = lengths_of<ROWS>(P, b);
-      w = __builtin_fmaf((float)r.tiles, (float)r.pages, w);
-    }
-    w = sum_wave(w) * (float)Hkv * P.per_part;
-    per = w < (float)UGBS_MAX_BLOCKS ? max((int)w + 1, P.min_pages) : UGBS_MAX_BLOCKS;
-    per = __builtin_amdgcn_readfirstlane(per);
+  if (B > kWaveBatch) {
+    const int b = __builtin_amdgcn_readfirstlane((ORDER == kJoinTiles ? P.schedule.join : P.schedule.part)[pos]);
+    if (b < 0) return false;
+    const int4 x = P.schedule.request[b];
+    const Lengths r = lengths_of<ROWS>(P, b);
+    out->b = b;
+    out->q = r.q;
+    out->kv = r.kv;
+    out->splits = x.y;
+    locate<ORDER>(P, pos - (ORDER == kJoinTiles ? x.w : x.x), r.tiles, x.z, out);
+    return true;
   }
+  constexpr int NC = kWaveBatch / 64;
+  Lengths r[NC];
+  float work = 0.f;
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    r[k] = Lengths{0, 0, 0, 0};
+    if (64 * k + lane < B) r[k] = lengths_of<ROWS>(P, 64 * k + lane);
+  }
+#pragma unroll
+  for (int k = 0; k < NC; ++k) work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
+  const int per = __builtin_amdgcn_readfirstlane(pages_per_part(P, sum_wave(work)));
   int before = 0, slots = 0;
-  for (int c = 0; c < B; c += 64) {
-    Lengths r{0, 0, 0, 0};
-    int splits = 1;
-    if (c + lane < B) {
-      r = lengths_of<ROWS>(P, c + lane);
-      if (P.splits && r.pages > per) splits = (r.pages + per - 1) / per;
-    }
-    const int units = r.tiles * Hkv;
+#pragma unroll
+  for (int k = 0; k < NC; ++k) {
+    if (64 * k >= B) return false;
+    const int splits = splits_of(r[k], per), units = r[k].tiles * Hkv;
     const int used = splits > 1 ? units * splits : 0;
     const int mine = ORDER == kJoinTiles ? (splits > 1 ? units : 0) : units * splits;
     const int upto = before + scan_add(mine), slots_upto = slots + scan_add(used);
     const unsigned long long found = __ballot(pos >= upto - mine && pos < upto);
     if (found) {
       const int l = __builtin_ctzll(found);
-      out->b = c + l;
-      out->q = __builtin_amdgcn_readlane(r.q, l);
-      out->kv = __builtin_amdgcn_readlane(r.kv, l);
+      out->b = 64 * k + l;
+      out->q = __builtin_amdgcn_readlane(r[k].q, l);
+      out->kv = __builtin_amdgcn_readlane(r[k].kv, l);
       out->splits = __builtin_amdgcn_readlane(splits, l);
-      const int tiles = __builtin_amdgcn_readlane(r.tiles, l);
-      int at = pos - __builtin_amdgcn_readlane(upto - mine, l);
-      if (ORDER == kGroups) {
-        const int groups = Hkv * out->splits, dealt = groups / 8 * 8;
-        int group;
-        if (at < dealt * tiles) {
-          group = at / 8 / tiles * 8 + at % 8;
-          out->tile = at / 8 % tiles;
-        } else {
-          group = dealt + (at - dealt * tiles) / tiles;
-          out->tile = (at - dealt * tiles) % tiles;
-        }
-        out->split = group % out->splits;
-        out->kvh = group / out->splits;
-      } else {
-        out->split = 0;
-        if (ORDER == kParts) {
-          out->split = at % out->splits;
-          at /= out->splits;
-        }
-        out->tile = at % tiles;
-        out->kvh = at / tiles;
-      }
-      out->slot = __builtin_amdgcn_readlane(slots_upto - used, l) + (out->kvh * tiles + out->tile) * out->splits;
+      locate<ORDER>(P, pos - __builtin_amdgcn_readlane(upto - mine, l), __builtin_amdgcn_readlane(r[k].tiles, l),
+                    __builtin_amdgcn_readlane(slots_upto - used, l), out);
       return true;
     }
     before = __builtin_amdgcn_readlane(upto, 63);
@@ -158,7 +173,93 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
   return false;
 }
 
-// Pages that rows tile 16 .. + 15 see (the last row sees most).
+// The schedule of a large batch.  Every workgroup forms the sums over all requests (4 a
+// thread) and then finds the request of its share of the parts by bisection.
+constexpr int kScheduleThreads = 1024;
+template <int ROWS>
+__global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheAttendParams P, int entries) {
+  constexpr int PER = UGBS_MAX_REQUESTS / kScheduleThreads, NW = kScheduleThreads / 64;
+  __shared__ int s_parts[UGBS_MAX_REQUESTS], s_joins[UGBS_MAX_REQUESTS];
+  __shared__ int s_wave[3][NW];
+  __shared__ float s_work[NW];
+  const int tid = threadIdx.x, w = tid >> 6, B = P.s.B, Hkv = P.s.Hkv;
+  Lengths r[PER];
+  float work = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k;
+    r[k] = Lengths{0, 0, 0, 0};
+    if (b < B) r[k] = lengths_of<ROWS>(P, b);
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
+  work = sum_wave(work);
+  if ((tid & 63) == 0) s_work[w] = work;
+  __syncthreads();
+  work = 0.f;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) work += s_work[v];
+  const int per = pages_per_part(P, work);
+  int n[3] = {0, 0, 0};                     // parts, slots, split tiles
+  int splits[PER];
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    splits[k] = splits_of(r[k], per);
+    const int units = r[k].tiles * Hkv;
+    n[0] += units * splits[k];
+    if (splits[k] > 1) {
+      n[1] += units * splits[k];
+      n[2] += units;
+    }
+  }
+  int at[3];
+#pragma unroll
+  for (int x = 0; x < 3; ++x) {
+    const int in = scan_add(n[x]);
+    at[x] = in - n[x];
+    if ((tid & 63) == 63) s_wave[x][w] = in;
+  }
+  __syncthreads();
+  int total[3] = {0, 0, 0};
+#pragma unroll
+  for (int v = 0; v < NW; ++v)
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {
+      if (v < w) at[x] += s_wave[x][v];
+      total[x] += s_wave[x][v];
+    }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k;
+    if (b < B) {
+      s_parts[b] = at[0];
+      s_joins[b] = at[2];
+      if (blockIdx.x == 0) P.schedule.request[b] = make_int4(at[0], splits[k], at[1], at[2]);
+      const int units = r[k].tiles * Hkv;
+      at[0] += units * splits[k];
+      if (splits[k] > 1) {
+        at[1] += units * splits[k];
+        at[2] += units;
+      }
+    }
+  }
+  __syncthreads();
+  // the last request with sums[b] <= i (those without parts have the same sum as the next)
+  auto request_at = [&](const int* sums, int i) {
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (sums[mid] <= i) lo = mid;
+      else hi = mid - 1;
+    }
+    return lo;
+  };
+  for (int i = blockIdx.x * kScheduleThreads + tid; i < entries; i += gridDim.x * kScheduleThreads)
+    P.schedule.part[i] = i < total[0] ? request_at(s_parts, i) : -1;
+  if (blockIdx.x == 0 && tid < kTarget) P.schedule.join[tid] = tid < total[2] ? request_at(s_joins, tid) : -1;
+}
+
+// Pages that the rows of a tile see (the last row sees most).
 template <int ROWS>
 __device__ __forceinline__ int pages_seen(const CacheAttendParams& P, const Part& u) {
   const int last = min((u.tile + 1) * ROWS, u.q * P.s.G) - 1;
@@ -371,6 +472,17 @@ __global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) 
 
 inline int64_t tiles_bound(const CacheShape& s, int rows_of_a_tile) {
   return (int64_t)s.B * s.Hkv * (((int64_t)s.rows * s.G + rows_of_a_tile - 1) / rows_of_a_tile);
+}
+
+// Entries of a schedule's list of parts.
+inline int64_t schedule_entries(const CacheShape& s, int rows_of_a_tile) { return tiles_bound(s, rows_of_a_tile) + kTarget; }
+
+// Before the parts of a large batch.
+template <int ROWS>
+void launch_schedule(const CacheAttendParams& P, hipStream_t stream) {
+  if (P.s.B <= kWaveBatch) return;
+  const int64_t entries = schedule_entries(P.s, ROWS), want = (entries + 4 * kScheduleThreads - 1) / (4 * kScheduleThreads);
+  cache_schedule_kernel<ROWS><<<(unsigned)(want < 256 ? want : 256), kScheduleThreads, 0, stream>>>(P, (int)entries);
 }
 
 // Launches of the join, after the parts.

@@ -200,6 +200,7 @@ hipError_t attend_rows(const CacheAttendParams& P, hipStream_t stream) {
   constexpr int NW = 4, ROWS = 16 * RT;
 
   const int64_t units = tiles_bound(P.s, ROWS);
+  launch_schedule<ROWS>(P, stream);
   cache_attend_rows_kernel<D, DT, RT, NW><<<(unsigned)(units + (P.splits ? kTarget : 0)), 64 * NW, 0, stream>>>(P);
   if (P.splits) launch_join<D, ROWS>(P, stream);
   return hipGetLastError();
@@ -224,18 +225,35 @@ hipError_t attend(const CacheAttendParams& P, hipStream_t stream) {
 
 }  // namespace
 
-size_t cache_attend_workspace(const CacheShape& s) {
+// Workspace: the parts' sums, their (maximum, sum) pairs, and a large batch's schedule.
+static size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+static size_t schedule_at(const CacheShape& s) {
   return may_split(s) ? (size_t)kSlots * tile_rows(s) * (s.d * sizeof(float) + sizeof(float2)) : 0;
+}
+
+size_t cache_attend_workspace(const CacheShape& s) {
+  size_t n = schedule_at(s);
+  if (s.B > kWaveBatch)
+    n = align256(n) + align256(s.B * sizeof(int4)) + align256(schedule_entries(s, tile_rows(s)) * sizeof(int32_t)) +
+        kTarget * sizeof(int32_t);
+  return n;
 }
 
 hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uint8_t* cache, const float* scales,
                                const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, uint16_t* O,
                                void* workspace, hipStream_t stream) {
-  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, 1.0f / kTarget, min_pages(s.d)};
+  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, 1.0f / kTarget, min_pages(s.d)};
   P.scale_log2 = s.scale * 1.4426950408889634f;
   P.splits = may_split(s);
   P.part_o = static_cast<float*>(workspace);
   P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)kSlots * tile_rows(s) * s.d);
+  if (s.B > kWaveBatch) {
+    uint8_t* const at = static_cast<uint8_t*>(workspace) + align256(schedule_at(s));
+    P.schedule.request = reinterpret_cast<int4*>(at);
+    P.schedule.part = reinterpret_cast<int32_t*>(at + align256(s.B * sizeof(int4)));
+    P.schedule.join = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(P.schedule.part) +
+                                                 align256(schedule_entries(s, tile_rows(s)) * sizeof(int32_t)));
+  }
   const bool f8 = s.dtype == UGBS_E4M3;
   if (s.d == 64) return f8 ? attend<64, UGBS_E4M3>(P, stream) : attend<64, UGBS_INT8>(P, stream);
   if (s.d == 128) return f8 ? attend<128, UGBS_E4M3>(P, stream) : attend<128, UGBS_INT8>(P, stream);

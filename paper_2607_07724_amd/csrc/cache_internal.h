@@ -47,6 +47,22 @@ __host__ __device__ constexpr int value_at(int t, int c) {
   return (t >> 5) * 32 * D + (c >> 5) * 1024 + ((t >> 2) & 3) * 256 + (c & 15) * 16 + ((c >> 4) & 1) * 8 + ((t >> 4) & 1) * 4 + (t & 3);
 }
 
+template <int CTRL, int ROW_MASK>
+__device__ __forceinline__ int dpp(int x) {      // 0 where the lane has no source
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROW_MASK, 0xf, false);
+}
+
+// Sum over lanes 0 .. l (shifts within 16 lanes, then the last lane of a row to the next rows).
+__device__ __forceinline__ int scan_add(int x) {
+  x += dpp<0x111, 0xf>(x);
+  x += dpp<0x112, 0xf>(x);
+  x += dpp<0x114, 0xf>(x);
+  x += dpp<0x118, 0xf>(x);
+  x += dpp<0x142, 0xa>(x);
+  x += dpp<0x143, 0xc>(x);
+  return x;
+}
+
 // 16 bytes that are read once: not kept in the caches (a decode step over 300 MB:
 // 64 -> 57 us).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

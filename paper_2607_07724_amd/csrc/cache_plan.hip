@@ -48,16 +48,6 @@ __device__ __forceinline__ Request request_of(const PlanParams& P, int b) {
   return r;
 }
 
-__device__ __forceinline__ int wave_scan(int x) {   // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  return x;
-}
-
 __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
   extern __shared__ int s_sum[];            // [B] pages given back before request b, [B] needed before it
   __shared__ int s_wave[2][kThreads / 64];
@@ -66,13 +56,15 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
   int* const s_need = s_sum + B;
   const int per = (B + kThreads - 1) / kThreads;
   const int b0 = min(tid * per, B), b1 = min(b0 + per, B);
+  const int count = P.free_count[0];
   int back = 0, need = 0;
+#pragma unroll 4
   for (int b = b0; b < b1; ++b) {
     const Request r = request_of(P, b);
     back += r.back;
     need += r.need;
   }
-  const int back_in = wave_scan(back), need_in = wave_scan(need);
+  const int back_in = scan_add(back), need_in = scan_add(need);
   const int w = tid >> 6;
   if ((tid & 63) == 63) {
     s_wave[0][w] = back_in;
@@ -88,7 +80,7 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
     }
     back_all += s_wave[0][v];
   }
-  const int held0 = min(max(P.free_count[0], 0), P.s.n_pages);
+  const int held0 = min(max(count, 0), P.s.n_pages);
   const int stock = min(held0 + back_all, P.s.n_pages);      // free pages to take from
   int taken = 0;                                             // pages granted up to this thread's last request
   for (int b = b0; b < b1; ++b) {
@@ -128,26 +120,34 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
   };
   const int stride = gridDim.x * kThreads, first = blockIdx.x * kThreads + tid;
   for (int j = first; j < stock - held0; j += stride) P.free_pages[held0 + j] = returned(j);
+  // four slots a thread at a time, so that their loads are on their way together
   const int rows = P.s.rows, total = B * rows;
-  for (int at = first; at < total; at += stride) {
-    const int b = at / rows, i = at - b * rows;
-    const Request r = request_of(P, b);
-    int slot = -1;
-    if (i < r.q && (r.need == 0 || s_need[b] + r.need <= stock)) {
+  for (int base = blockIdx.x * 4 * kThreads + tid; base < total; base += 4 * stride) {
+    int place[4], from[4], page[4];
+    bool new_page[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = min(base + k * kThreads, total - 1), b = at / rows, i = at - b * rows;
+      const Request r = request_of(P, b);
       const int pos = r.ctx + i, p = pos / kBlock;
-      int32_t* const entry = P.table + (size_t)b * P.s.max_pages + p;
-      int page;
-      if (p < r.held) {
-        page = *entry;
-      } else {
-        const int from = stock - 1 - s_need[b] - (p - r.held);
-        page = from >= held0 ? returned(from - held0) : P.free_pages[from];
-        if (pos % kBlock == 0) *entry = page;
+      place[k] = i < r.q && (r.need == 0 || s_need[b] + r.need <= stock) ? pos : -1;
+      from[k] = stock - 1 - s_need[b] - (p - r.held);
+      new_page[k] = p >= r.held;
+      page[k] = -1;
+      if (place[k] >= 0) {
+        if (!new_page[k]) page[k] = P.table[(size_t)b * P.s.max_pages + p];
+        else page[k] = from[k] >= held0 ? returned(from[k] - held0) : P.free_pages[from[k]];
       }
-      // an entry that is no page gives no slot
-      if (page >= 0 && page < P.s.n_pages) slot = page * kBlock + pos % kBlock;
     }
-    P.slots[at] = slot;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int at = base + k * kThreads;
+      if (at >= total) break;
+      if (place[k] >= 0 && new_page[k] && place[k] % kBlock == 0)
+        P.table[(size_t)(at / rows) * P.s.max_pages + place[k] / kBlock] = page[k];
+      // an entry that is no page gives no slot
+      P.slots[at] = place[k] >= 0 && page[k] >= 0 && page[k] < P.s.n_pages ? page[k] * kBlock + place[k] % kBlock : -1;
+    }
   }
 }
 
@@ -159,7 +159,7 @@ hipError_t launch_cache_plan(const CacheShape& s, const int32_t* ctx_lens, const
   const PlanParams P{s, ctx_lens, new_lens, free_pages, free_count, table, kv_lens, q_lens, slots, free_left};
   const int64_t items = (int64_t)s.B * s.rows;
   const int64_t want = (items + 4 * kThreads - 1) / (4 * kThreads);
-  const unsigned grid = (unsigned)(want < 256 ? want : 256);
+  const unsigned grid = (unsigned)(want < 1024 ? want : 1024);
   cache_plan_kernel<<<grid, kThreads, 2 * sizeof(int) * s.B, stream>>>(P);
   return hipGetLastError();
 }

@@ -247,6 +247,7 @@ hipError_t tiles(const CacheAttendParams& P, hipStream_t stream) {
   constexpr int NW = 4, ROWS = 16 * RT;
   static_assert(ROWS == tile_rows_many(D), "rows of a tile");
   const int64_t units = tiles_bound(P.s, ROWS);
+  launch_schedule<ROWS>(P, stream);
   const unsigned grid = (unsigned)(units + (P.splits ? kTarget : 0));
   if ((int64_t)P.s.rows * P.s.G <= ROWS) cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true><<<grid, 64 * NW, 0, stream>>>(P);
   else cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false><<<grid, 64 * NW, 0, stream>>>(P);

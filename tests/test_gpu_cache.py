@@ -371,11 +371,16 @@ def test_long_requests_are_split_and_joined(rows, H, Hkv, d, dtype, lens):
     check_attend(g, lens, [min(rows, n) for n in lens], rows, H, Hkv, d, dtype, max_pages=4096)
 
 
-def test_many_requests_among_them_a_long_one():
-    g = np.random.default_rng(21)
-    lens = [int(n) for n in g.integers(0, 200, 300)]
-    lens[137] = 9000
-    check_attend(g, lens, [min(1, n) for n in lens], 1, 4, 2, 64, 0, max_pages=200)
+@pytest.mark.parametrize("B,rows,H,Hkv,d,dtype,longest", [
+    (64, 1, 4, 2, 64, 0, 9000), (65, 1, 4, 2, 64, 0, 0), (256, 1, 4, 1, 64, 1, 5000), (257, 1, 4, 2, 64, 0, 9000),
+    (300, 9, 4, 1, 64, 0, 3000), (300, 3, 8, 1, 128, 0, 0), (700, 20, 2, 1, 64, 1, 2500), (4096, 1, 2, 1, 64, 0, 1500)])
+def test_many_requests_among_them_a_long_one(B, rows, H, Hkv, d, dtype, longest):
+    g = np.random.default_rng(B + rows)
+    lens = [int(n) for n in g.integers(0, 130 if B > 500 else 200, B)]
+    lens[B // 2 + 7] = longest
+    q = [int(min(n, m)) for n, m in zip(lens, g.integers(0, rows + 1, B))]
+    q[B // 2 + 7] = min(rows, longest)
+    check_attend(g, lens, q, rows, H, Hkv, d, dtype, max_pages=200)
 
 
 def test_sharp_and_flat_softmax():
