@@ -295,16 +295,21 @@ struct Pages {
     scale = make_float2(0.f, 0.f);
     if (left >> lane & 1) scale = *reinterpret_cast<const float2*>(scales + (size_t)id * stride);
   }
-  // the next lane to visit, -1: none; the lanes may then be others
-  __device__ __forceinline__ int next() {
-    if (!left && first + 64 * step < end) {
+  __device__ __forceinline__ void advance() {      // the next 64, if there are any
+    if (first + 64 * step < end) {
       first += 64 * step;
       load();
     }
-    if (!left) return -1;
+  }
+  __device__ __forceinline__ int pop() {
     const int l = __builtin_ctzll(left);
     left &= left - 1;
     return l;
+  }
+  // the next lane to visit, -1: none; the lanes may then be others
+  __device__ __forceinline__ int next() {
+    if (!left) advance();
+    return left ? pop() : -1;
   }
   __device__ __forceinline__ int page(int l) const { return __builtin_amdgcn_readlane(id, l); }
   __device__ __forceinline__ int at(int l) const { return first + step * l; }

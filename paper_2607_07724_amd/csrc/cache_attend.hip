@@ -18,6 +18,8 @@
 // up the call.  The lengths are on the device; each wave forms the sums over
 // the requests for itself.  Parts leave their sums and maxima in the workspace,
 // and a second launch joins them, in the order of the pages.
+#include <type_traits>
+
 #include "cache_attend.h"
 
 namespace ugbs {
@@ -48,6 +50,10 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   const int p0 = __builtin_amdgcn_readfirstlane(n * u.split / u.splits);
   const int p1 = __builtin_amdgcn_readfirstlane(n * (u.split + 1) / u.splits);
 
+  // waves 2 j and 2 j + 1 take the halves of pages p0 + j, p0 + j + NW / 2, ...
+  const int half = w & 1;
+  Pages pages = pages_of(P, u, p0, p1, w >> 1, NW / 2);
+
   // this lane's rows: the last key each sees, and its query
   int last[RT];
   bf16x8 bq[RT][2 * (D / 64)];
@@ -70,18 +76,17 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   // every valid row sees the keys up to here
   const int all_see = u.kv - u.q + u.tile * ROWS / s.G;
 
-  const int32_t* const row = P.table + (size_t)u.b * s.max_pages;
   uint4 kx[L], vx[L];
-  auto half_of = [&](int page, int at) {
-    return reinterpret_cast<const uint4*>(P.cache + ((size_t)page * s.Hkv + u.kvh) * 2 * (kBlock * D) + (at & 1) * 32 * D) + lane;
+  auto bytes_of = [&](int page) {
+    return reinterpret_cast<const uint4*>(P.cache + ((size_t)page * s.Hkv + u.kvh) * 2 * (kBlock * D) + half * 32 * D) + lane;
   };
-  auto fetch_k = [&](int page, int at) {
-    const uint4* const src = half_of(page, at);
+  auto fetch_k = [&](int page) {
+    const uint4* const src = bytes_of(page);
 #pragma unroll
     for (int e = 0; e < L; ++e) kx[e] = load_once(src + 64 * e);
   };
-  auto fetch_v = [&](int page, int at) {
-    const uint4* const src = half_of(page, at) + kBlock * D / 16;
+  auto fetch_v = [&](int page) {
+    const uint4* const src = bytes_of(page) + kBlock * D / 16;
 #pragma unroll
     for (int e = 0; e < L; ++e) vx[e] = load_once(src + 64 * e);
   };
@@ -96,27 +101,12 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
     l_run[rt] = 0.f;
   }
 
-  // half pages at, at + NW, ... of the request; those in no page are passed over
-  const int end = 2 * p1;
-  auto next_half = [&](int at, int* page) {
-    for (; at < end; at += NW) {
-      *page = __builtin_amdgcn_readfirstlane(row[at >> 1]);
-      if (*page >= 0 && *page < s.n_pages) break;
-    }
-    return at;
-  };
-  int page = 0, page2 = 0;
-  int at = next_half(2 * p0 + w, &page);
-  if (at < end) {
-    fetch_k(page, at);
-    fetch_v(page, at);
-  }
-  const int key_first = at < end ? 32 * at : INT32_MAX;     // the first position this wave sees
-  while (at < end) {
-    const int key0 = 32 * at;               // position of the half page's first token
-    const float* const sc_page = P.scales + 2 * ((size_t)page * s.Hkv + u.kvh);
-    const float f = sc_page[0] * P.scale_log2, vs = sc_page[1];
-    const int at2 = next_half(at + NW, &page2);
+  // One half page; MORE: another one follows, whose loads go out here.  (The last one is a
+  // step of its own: loads behind a condition would make every wait one for all of them.)
+  auto step = [&](int l, int next, auto more_tag) {
+    constexpr bool MORE = decltype(more_tag)::value;
+    const int key0 = kBlock * pages.at(l) + 32 * half;      // position of the half page's first token
+    const float f = pages.key_scale(l) * P.scale_log2, vs = pages.value_scale(l);
     f32x4 sc[RT][2];
 #pragma unroll
     for (int kt = 0; kt < 2; ++kt) {
@@ -133,7 +123,7 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
         }
       }
     }
-    if (at2 < end) fetch_k(page2, at2);
+    if constexpr (MORE) fetch_k(pages.page(next));
     const bool edge = key0 + 31 > all_see;
     bf16x8 bp[RT];
 #pragma unroll
@@ -182,9 +172,21 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
         acc[rt][2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, bp[rt], acc[rt][2 * e + 1], 0, 0, 0);
       }
     }
-    if (at2 < end) fetch_v(page2, at2);
-    at = at2;
-    page = page2;
+    if constexpr (MORE) fetch_v(pages.page(next));
+  };
+  int key_first = INT32_MAX;                // the first position this wave sees
+  while (pages.left) {
+    int l = pages.pop();
+    fetch_k(pages.page(l));
+    fetch_v(pages.page(l));
+    key_first = min(key_first, kBlock * pages.at(l) + 32 * half);
+    while (pages.left) {
+      const int next = pages.pop();
+      step(l, next, std::true_type{});
+      l = next;
+    }
+    step(l, 0, std::false_type{});
+    pages.advance();
   }
 
   bool seen[RT];
