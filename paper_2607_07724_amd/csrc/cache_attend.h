@@ -8,7 +8,7 @@ namespace ugbs {
 // Parts a call aims at, at most, and the pages of a part, at least: 128 KiB.
 constexpr int kTarget = 512;
 constexpr int min_pages(int d) { return 1024 / d; }
-// Every split tile has at least two parts, and parts of split tiles are at most twice W / X, X > W / target.
+// Parts of split tiles are at most twice W / X, X > W / kTarget, and a split tile has at least two.
 constexpr int kSlots = 2 * kTarget;
 
 // Where the parts lie, of batches of more than kWaveBatch requests: formed once by
@@ -35,7 +35,6 @@ struct CacheAttendParams {
   float scale_log2;
   bool splits;        // parts are allowed
   Schedule schedule;  // of more than kWaveBatch requests
-  float per_part;     // 1 / parts aimed at (at most kTarget, a power of two)
   int min_pages;
 };
 
@@ -81,11 +80,18 @@ struct Part {
   int b, kvh, tile, split, splits, slot, q, kv;   // slot: of the tile's first part
 };
 
-// Pages per part, from the sum over the requests of tiles times pages (fp32, added in
-// the same order wherever it is formed; + 1 covers the rounding, X being at most 4096).
-__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work) {
+// Pages per part, from the sums over the requests of tiles times pages and of tiles
+// (fp32, added in the same order wherever they are formed; + 1 covers the rounding, X
+// being at most 4096).  Each tile ends with a part that is not full, so kTarget is missed
+// by less than the tiles.  Where kTarget parts are what the chip holds at once (two a CU:
+// more than 16 rows) the tiles are taken off, down to half of it: 56 tiles as 560 parts
+// took two rounds, 264 us for 222.  With 16 rows four parts fit a CU, and the more the
+// better (32 ragged requests: 57 us, with half the parts 63).
+template <int ROWS>
+__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles) {
   if (!P.splits) return UGBS_MAX_BLOCKS;
-  const float x = work * (float)P.s.Hkv * P.per_part;
+  const float aim = ROWS == 16 ? (float)kTarget : fmaxf((float)kTarget - tiles * (float)P.s.Hkv, 0.5f * kTarget);
+  const float x = work * (float)P.s.Hkv / aim;
   return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, P.min_pages) : UGBS_MAX_BLOCKS;
 }
 __device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.pages > per ? (r.pages + per - 1) / per : 1; }
@@ -109,6 +115,7 @@ __device__ __forceinline__ void locate(const CacheAttendParams& P, int at, int t
       group = dealt + (at - dealt * tiles) / tiles;
       out->tile = (at - dealt * tiles) % tiles;
     }
+    out->tile = tiles - 1 - out->tile;      // later rows see more: first
     out->split = group % out->splits;
     out->kvh = group / out->splits;
   } else {
@@ -126,6 +133,7 @@ template <int ROWS, Order ORDER>
 __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
   const int lane = threadIdx.x & 63, B = P.s.B, Hkv = P.s.Hkv;
   if (B > kWaveBatch) {
+    if (ORDER == kJoinTiles && pos >= kTarget) return false;
     const int b = __builtin_amdgcn_readfirstlane((ORDER == kJoinTiles ? P.schedule.join : P.schedule.part)[pos]);
     if (b < 0) return false;
     const int4 x = P.schedule.request[b];
@@ -139,15 +147,18 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
   }
   constexpr int NC = kWaveBatch / 64;
   Lengths r[NC];
-  float work = 0.f;
+  float work = 0.f, tiles = 0.f;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
     r[k] = Lengths{0, 0, 0, 0};
     if (64 * k + lane < B) r[k] = lengths_of<ROWS>(P, 64 * k + lane);
   }
 #pragma unroll
-  for (int k = 0; k < NC; ++k) work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
-  const int per = __builtin_amdgcn_readfirstlane(pages_per_part(P, sum_wave(work)));
+  for (int k = 0; k < NC; ++k) {
+    work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
+    tiles += (float)r[k].tiles;
+  }
+  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, sum_wave(work), ROWS == 16 ? 0.f : sum_wave(tiles)));
   int before = 0, slots = 0;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
@@ -181,10 +192,10 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
   constexpr int PER = UGBS_MAX_REQUESTS / kScheduleThreads, NW = kScheduleThreads / 64;
   __shared__ int s_parts[UGBS_MAX_REQUESTS], s_joins[UGBS_MAX_REQUESTS];
   __shared__ int s_wave[3][NW];
-  __shared__ float s_work[NW];
+  __shared__ float2 s_work[NW];
   const int tid = threadIdx.x, w = tid >> 6, B = P.s.B, Hkv = P.s.Hkv;
   Lengths r[PER];
-  float work = 0.f;
+  float work = 0.f, tiles = 0.f;
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int b = PER * tid + k;
@@ -192,14 +203,21 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
     if (b < B) r[k] = lengths_of<ROWS>(P, b);
   }
 #pragma unroll
-  for (int k = 0; k < PER; ++k) work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
+  for (int k = 0; k < PER; ++k) {
+    work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
+    tiles += (float)r[k].tiles;
+  }
   work = sum_wave(work);
-  if ((tid & 63) == 0) s_work[w] = work;
+  tiles = sum_wave(tiles);
+  if ((tid & 63) == 0) s_work[w] = make_float2(work, tiles);
   __syncthreads();
-  work = 0.f;
+  work = tiles = 0.f;
 #pragma unroll
-  for (int v = 0; v < NW; ++v) work += s_work[v];
-  const int per = pages_per_part(P, work);
+  for (int v = 0; v < NW; ++v) {
+    work += s_work[v].x;
+    tiles += s_work[v].y;
+  }
+  const int per = pages_per_part<ROWS>(P, work, tiles);
   int n[3] = {0, 0, 0};                     // parts, slots, split tiles
   int splits[PER];
 #pragma unroll
@@ -401,78 +419,91 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
   }
 }
 
-// Joins the parts of one row: a workgroup per (split tile, row), D / 4 threads to
-// a part, the parts round the others.  The first kAhead parts of a thread are on
-// their way before the weights are known (latency is all there is here).
-constexpr int kJoin = 256;
-template <int D, int ROWS>
-__global__ void __launch_bounds__(kJoin) cache_join_kernel(CacheAttendParams P) {
-  constexpr int CG = D / 4, GR = kJoin / CG, kAhead = 8;
-  __shared__ float2 s_part[kSlots];         // maximum, then weight; sum
+// Joins the parts of split tiles: D / 4 threads to a row and part, the parts of a row
+// round its threads; the first kAhead parts of a thread are on their way before the
+// weights are known.  Few rows in all (JR 1): a workgroup for each row that there could
+// be.  Many (JR 4): four rows of a tile at a time, by workgroups that go on to the next
+// four (a workgroup for each row took 16 us at 64 rows a tile where nothing was split).
+template <int D, int ROWS, int JR>
+__global__ void __launch_bounds__(JR == 1 ? 256 : 512) cache_join_kernel(CacheAttendParams P, int row_groups, int items) {
+  constexpr int kJoin = JR == 1 ? 256 : 512, kJoinRows = JR;
+  constexpr int CG = D / 4, GR = kJoin / kJoinRows / CG, kAhead = 8;
+  constexpr int TR = kJoin / kJoinRows;     // threads of a row
+  __shared__ float2 s_part[kJoinRows][kSlots / 2];   // maximum, then weight; sum
   __shared__ float2 s_ml[kJoin / 64];
-  __shared__ f32x4 s_o[GR][CG];
-  Part u;
-  if (!find_part<ROWS, kJoinTiles>(P, blockIdx.x, &u)) return;
+  __shared__ f32x4 s_o[GR][kJoinRows][CG];
+  static_assert(TR % 64 == 0 && GR * CG == TR, "whole waves to a row");
   const CacheShape& s = P.s;
-  const int tid = threadIdx.x, w = tid >> 6, rr = blockIdx.y, at_row = u.tile * ROWS + rr;
-  if (at_row >= u.q * s.G) return;
-  const int gr = tid / CG, c = tid % CG;
-  const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
-  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
-  float M = -__builtin_huge_valf();
-  for (int v = tid; v < u.splits; v += kJoin) {
-    s_part[v] = ml[(size_t)v * ROWS];
-    M = fmaxf(M, s_part[v].x);
-  }
-  f32x4 ahead[kAhead];
+  const int tid = threadIdx.x, w = tid >> 6;
+  const int jr = tid / TR, tr = tid % TR, gr = tr / CG, c = tr % CG;
+  int item = blockIdx.x;
+  do {
+    Part u;
+    if (!find_part<ROWS, kJoinTiles>(P, JR == 1 ? item : item / row_groups, &u)) return;
+    const int rr = JR == 1 ? blockIdx.y : item % row_groups * kJoinRows + jr, at_row = u.tile * ROWS + rr;
+    const bool ok = at_row < u.q * s.G;
+    const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
+    const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
+    if (JR == 1 && !ok) return;            // the whole workgroup's row
+    const int splits = ok ? u.splits : 0;   // of this thread's row
+    float M = -__builtin_huge_valf();
+    for (int v = tr; v < splits; v += TR) {
+      s_part[jr][v] = ml[(size_t)v * ROWS];
+      M = fmaxf(M, s_part[jr][v].x);
+    }
+    f32x4 ahead[kAhead];
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k) {
-    const int v = gr + k * GR;
-    ahead[k] = po[(size_t)min(v, u.splits - 1) * (ROWS * CG)];
-  }
+    for (int k = 0; k < kAhead; ++k) {
+      const int v = gr + k * GR;
+      ahead[k] = splits > 0 ? po[(size_t)min(v, splits - 1) * (ROWS * CG)] : f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
-  if ((tid & 63) == 0) s_ml[w].x = M;
-  __syncthreads();
+    for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
+    if ((tid & 63) == 0) s_ml[w].x = M;
+    __syncthreads();
 #pragma unroll
-  for (int v = 0; v < kJoin / 64; ++v) M = fmaxf(M, s_ml[v].x);
-  float l = 0.f;
-  for (int v = tid; v < u.splits; v += kJoin) {
-    const float2 x = s_part[v];
-    // a part that saw none of the row's keys weighs nothing
-    const float a = x.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(x.x - M);
-    s_part[v].x = a;
-    if (a != 0.f) l += a * x.y;
-  }
-  l = sum_wave(l);
-  if ((tid & 63) == 0) s_ml[w].y = l;
-  __syncthreads();
-  l = 0.f;
+    for (int v = 0; v < TR / 64; ++v) M = fmaxf(M, s_ml[jr * (TR / 64) + v].x);
+    float l = 0.f;
+    for (int v = tr; v < splits; v += TR) {
+      const float2 x = s_part[jr][v];
+      // a part that saw none of the row's keys weighs nothing
+      const float a = x.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(x.x - M);
+      s_part[jr][v].x = a;
+      if (a != 0.f) l += a * x.y;
+    }
+    l = sum_wave(l);
+    if ((tid & 63) == 0) s_ml[w].y = l;
+    __syncthreads();
+    l = 0.f;
 #pragma unroll
-  for (int v = 0; v < kJoin / 64; ++v) l += s_ml[v].y;
-  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto add = [&](int v, const f32x4& x) {
-    const float a = s_part[v].x;
+    for (int v = 0; v < TR / 64; ++v) l += s_ml[jr * (TR / 64) + v].y;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](int v, const f32x4& x) {
+      const float a = s_part[jr][v].x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] += a * x[e];
-  };
+      for (int e = 0; e < 4; ++e) o[e] += a * x[e];
+    };
 #pragma unroll
-  for (int k = 0; k < kAhead; ++k)
-    if (gr + k * GR < u.splits) add(gr + k * GR, ahead[k]);
+    for (int k = 0; k < kAhead; ++k)
+      if (gr + k * GR < splits) add(gr + k * GR, ahead[k]);
 #pragma unroll 4
-  for (int v = gr + kAhead * GR; v < u.splits; v += GR) add(v, po[(size_t)v * (ROWS * CG)]);
-  s_o[gr][c] = o;
-  __syncthreads();
-  if (gr == 0) {
+    for (int v = gr + kAhead * GR; v < splits; v += GR) add(v, po[(size_t)v * (ROWS * CG)]);
+    s_o[gr][jr][c] = o;
+    __syncthreads();
+    if (gr == 0 && ok) {
 #pragma unroll
-    for (int v = 1; v < GR; ++v)
+      for (int v = 1; v < GR; ++v)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += s_o[v][c][e];
-    const float inv = reciprocal(M, l);
-    const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
-    *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + 4 * c) =
-        make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-  }
+        for (int e = 0; e < 4; ++e) o[e] += s_o[v][jr][c][e];
+      const float inv = reciprocal(M, l);
+      const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
+      *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + 4 * c) =
+          make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+    }
+    if (JR == 1) return;
+    __syncthreads();                        // the next rows use the same LDS
+    item += gridDim.x;
+  } while (item < items);
 }
 
 inline int64_t tiles_bound(const CacheShape& s, int rows_of_a_tile) {
@@ -493,9 +524,15 @@ void launch_schedule(const CacheAttendParams& P, hipStream_t stream) {
 // Launches of the join, after the parts.
 template <int D, int ROWS>
 void launch_join(const CacheAttendParams& P, hipStream_t stream) {
-  const int64_t units = tiles_bound(P.s, ROWS), rows = (int64_t)P.s.rows * P.s.G;
-  const dim3 grid((unsigned)(units < kTarget ? units : kTarget), (unsigned)(rows < ROWS ? rows : ROWS));
-  cache_join_kernel<D, ROWS><<<grid, kJoin, 0, stream>>>(P);
+  const int64_t all_rows = (int64_t)P.s.rows * P.s.G, all_tiles = tiles_bound(P.s, ROWS);
+  const int rows = (int)(all_rows < ROWS ? all_rows : ROWS);             // of a tile
+  const int tiles = (int)(all_tiles < kTarget ? all_tiles : kTarget);    // at most kTarget are split
+  if (tiles * rows <= 8192) {
+    cache_join_kernel<D, ROWS, 1><<<dim3(tiles, rows), 256, 0, stream>>>(P, 0, 0);
+  } else {
+    const int groups = (rows + 3) / 4;
+    cache_join_kernel<D, ROWS, 4><<<512, 512, 0, stream>>>(P, groups, tiles * groups);
+  }
 }
 
 }  // namespace

@@ -244,7 +244,7 @@ size_t cache_attend_workspace(const CacheShape& s) {
 hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uint8_t* cache, const float* scales,
                                const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, uint16_t* O,
                                void* workspace, hipStream_t stream) {
-  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, 1.0f / kTarget, min_pages(s.d)};
+  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, min_pages(s.d)};
   P.scale_log2 = s.scale * 1.4426950408889634f;
   P.splits = may_split(s);
   P.part_o = static_cast<float*>(workspace);
