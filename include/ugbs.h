@@ -497,7 +497,7 @@ UGBS_API int ugbs_cache_plan(const ugbs_cache* c, const int32_t* ctx_lens, const
  *           of the page, or token 0 of another page).  A row whose slot breaks
  *           this, or lies in no page, is not stored; where it would be the first
  *           one in its page, the page's others aren't either.  Rows without a slot
- *           are not read.  No two requests may add to the same page.
+ *           are not stored.  No page may take rows twice in a call, from one request or two.
  *   The scale of a page (per kv head, for keys and for values) is the smallest
  *   power of two s >= 2^-100 with max |x| <= M s over the tokens it was given, M =
  *   448 (e4m3) or 127.  Bytes are x / s, rounded once to nearest, ties to even.
@@ -513,7 +513,8 @@ UGBS_API int ugbs_cache_store(const ugbs_cache* c, const void* K, const void* V,
  *   count : [B] int32, positions read (taken as 0..width).
  *   width : rows of K and V, 1..UGBS_MAX_WIDTH.
  *   K, V  : [B, H_kv, width, d] bf16, 16-byte aligned: row i < count[b] gets
- *           position start[b] + i; the other rows are left as they are.  A
+ *           position start[b] + i; the other rows are left as they are, and K
+ *           and V must not overlap.  A
  *           position in no page, or behind the table, gives 0. */
 UGBS_API int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float* scales, const int32_t* table,
                              const int32_t* start, const int32_t* count, int32_t width, void* K, void* V,

@@ -618,7 +618,8 @@ class CacheBuffers:
 
 class CacheStep:
     """What the layers of a step share: table, free pages, lengths, slots and the attention's workspace
-    (allocated by torch).  At first all pages are free and all requests empty."""
+    (allocated by torch).  At first all pages are free and all requests empty.  Made for the `rows` of `c`;
+    a step may be planned with fewer (single tokens after prompts)."""
 
     def __init__(self, c: Cache, device="cuda"):
         import torch
@@ -633,13 +634,19 @@ class CacheStep:
         self.ctx_lens, self.free_count = self._before[:B], self._before[B:]
         self.kv_lens, self.free_left = self._after[:B], self._after[B:]
         self.q_lens = torch.zeros((B,), **i32)
-        self.slots = torch.full((B, c.rows), -1, **i32)
+        self._slots = torch.full((B * c.rows,), -1, **i32)
+        self.slots = self._slots.view(B, c.rows)
         self.workspace = torch.empty((max(ugbs_cache_workspace_bytes(c), 256),), dtype=torch.uint8, device=device)
 
     def plan(self, c: Cache, new_lens, stream=None):
         """A step: every request goes on from its kv_lens with new_lens [B] int32 tokens.  Called once, before
-        the step's layers, on the current stream (or `stream`, as the layers' calls)."""
+        the step's layers, on the current stream (or `stream`, as the layers' calls).  `c` is the layers' too:
+        its `rows` give the shape of `slots`."""
         torch = _get_torch()
+        n = c.batch * c.rows
+        if n > self._slots.numel():
+            raise ValueError(f"the step was made for at most {self._slots.numel() // c.batch} rows, not {c.rows}")
+        self.slots = self._slots[:n].view(c.batch, c.rows)
         if stream is None:
             torch.add(self._after, 0, out=self._before)
         else:
@@ -652,6 +659,8 @@ class CacheStep:
 def prefill_cached(p: Problem, c: Cache, Q, K, V, O, bufs: Buffers, cbufs: CacheBuffers, step: CacheStep, stream=None):
     """prefill of prompts that begin with this step, their K and V kept in the cache (c.rows == p.seq_len;
     step.plan comes first)."""
+    if c.rows != p.seq_len:
+        raise ValueError(f"the cache's rows ({c.rows}) are not the prompt's {p.seq_len}")
     prefill(p, Q, K, V, O, bufs, stream)
     ugbs_cache_store(c, K, V, step.slots, cbufs.cache, cbufs.scales, stream)
     return O

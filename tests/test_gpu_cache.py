@@ -525,16 +525,15 @@ def test_prompts_then_tokens_then_other_requests(dtype):
     ugbs.prefill(p, *t, O2, ugbs.Buffers(p))
     assert torch.equal(O.view(torch.int16), O2.view(torch.int16))      # the prefill itself is what it was
     mir.step(new, K, V, N)
+    with pytest.raises(ValueError):
+        step.plan(ugbs.Cache.make(B, H, Hkv, d, 14, 8, rows=N + 1), dev(new))
+    with pytest.raises(ValueError):
+        ugbs.prefill_cached(p, ugbs.Cache.make(B, H, Hkv, d, 14, 8, rows=64), *t, O, None, cbufs, step)
     for rows, new in ((1, [1, 1]), (1, [1, 1]), (5, [5, 2]), (1, [1, -1]), (70, [70, 60]), (70, [70, 70]), (1, [1, 0])):
         c = ugbs.Cache.make(B, H, Hkv, d, 14, 8, rows=rows, dtype=dtype)
         Qb, Qv = bf16(g.normal(0, 1, (B, H, rows, d)))
         Kb, K = bf16(g.normal(0, 2.0, (B, Hkv, rows, d)))
         Vb, V = bf16(g.normal(0, 2.0, (B, Hkv, rows, d)))
-        nxt = ugbs.CacheStep(c)
-        for name in ("table", "free_pages"):
-            getattr(nxt, name).copy_(getattr(step, name))
-        nxt._after.copy_(step._after)
-        step = nxt
         step.plan(c, dev(np.array(new, I32)))
         O = torch.zeros((B, H, rows, d), dtype=torch.bfloat16, device="cuda")
         ugbs.cache_layer(c, dev_bf16(Qb), dev_bf16(Kb), dev_bf16(Vb), O, cbufs, step)
