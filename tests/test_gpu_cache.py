@@ -280,13 +280,16 @@ def test_load_behind_the_table_gives_zeros():
 
 # ---------------------------------------------------------------- attention
 
-def reference(x, b, Qv, kv, q, scale):
+def reference(x, b, Qv, kv, q, scale, tiles=False):
     """The oracle's O [H, q, d] and how far the kernel's may be off, elementwise.
 
     With p the probabilities: their rounding to bf16 is off by 2^-8 of each; a score is a sum of d fp32
     products and three more fp32 roundings, off by (d + 3) 2^-24 sum |q k| scale, which moves p, and the
     sum that divides it, by as much, relatively (e^x - 1 <= 1.01 x here); the exponential, the scale by
-    2^x of a moved maximum and the sums over n keys add (n + 64) 2^-24; the result's rounding 2^-8 |O|."""
+    2^x of a moved maximum and the sums over n keys add (n + 64) 2^-24; the result's rounding 2^-8 |O|.
+
+    tiles (many rows, e4m3, d 128 and 256): a query channel is two e4m3 numbers, off by 2^-22 of the
+    largest of the 32 channels (in a row) that share a scale."""
     k, v, there = x.tokens(b, max(kv, 0))
     O = co.attend(Qv, k, v, there, kv, q, scale)
     H, G = Qv.shape[0], Qv.shape[0] // k.shape[0]
@@ -301,6 +304,9 @@ def reference(x, b, Qv, kv, q, scale):
             p = np.exp(s - s.max())
             p /= p.sum()
             spread = (np.abs(kk) @ np.abs(Qv[h, i])).max() * scale
+            if tiles and x.d >= 128 and x.dtype == ugbs.E4M3:
+                m = np.repeat(np.abs(Qv[h, i]).reshape(x.d // 32, 32).max(1), 32)
+                spread += 2.0 ** -22 / (x.d + 3) * 2.0 ** 24 * (np.abs(kk) @ m).max() * scale
             rel = 2.0 ** -8 + 2.02 * (x.d + 3) * 2.0 ** -24 * spread + (len(seen) + 64) * 2.0 ** -24
             tol[h, i] = rel * (p @ np.abs(v[h // G][seen])) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(O[h, i]) + 1e-30
     return O, tol
@@ -316,19 +322,19 @@ def run_attend(c, x, Qb, kv, q, workspace=True, fill=7.0):
     return O
 
 
-def check_attend(g, lens, q, rows, H, Hkv, d, dtype, max_pages=None, scale=0.0, spoil=None, loud=1.0, temper=1.0):
+def check_attend(g, lens, q, rows, H, Hkv, d, dtype, max_pages=None, scale=0.0, spoil=None, loud=1.0, temper=1.0, channels=1.0):
     x = Contents(g, lens, Hkv, d, dtype, max_pages=max_pages, loud=loud)
     if spoil:
         spoil(x)
     B = len(lens)
-    Qb, Qv = bf16(g.normal(0, temper, (B, H, rows, d)))
+    Qb, Qv = bf16(g.normal(0, temper, (B, H, rows, d)) * channels)
     for b in range(B):
         Qb[b, :, q[b]:] = 0x7FC0                   # rows without a token are not read
     c = ugbs.Cache.make(B, H, Hkv, d, x.n_pages, x.max_pages, rows=rows, dtype=dtype, scale=scale)
     O = run_attend(c, x, Qb, lens, q)
     got = bf16_to_f64(host_bits(O))
     for b in range(B):
-        want, tol = reference(x, b, Qv[b], lens[b], q[b], scale or 1 / math.sqrt(d))
+        want, tol = reference(x, b, Qv[b], lens[b], q[b], scale or 1 / math.sqrt(d), rows * H // Hkv > (32 if d < 256 else 16))
         off = np.abs(got[b, :, :q[b]] - want[:, :q[b]])
         assert (off <= tol[:, :q[b]]).all(), (b, float((off - tol[:, :q[b]]).max()), np.argwhere(~(off <= tol[:, :q[b]]))[:3])
         assert (got[b, :, q[b]:] == 7.0).all(), b
@@ -389,6 +395,22 @@ def test_sharp_and_flat_softmax():
         g = np.random.default_rng(5)
         check_attend(g, [500, 64, 1000], [1, 1, 1], 1, 4, 1, 128, 0, temper=temper)
         check_attend(g, [500, 640], [100, 30], 100, 4, 1, 128, 1, temper=temper)
+
+
+@pytest.mark.parametrize("d", [128, 256])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_channels_of_very_different_size(rows, d):
+    """Query channels from 1 to 2^-17 of the largest, and keys that make up for some of it."""
+    g = np.random.default_rng(d + rows)
+    channels = 2.0 ** -g.integers(0, 18, d) * 30
+
+    def spoil(x):                                  # the loudest quarter of the channels has keys of 0
+        k, v = co.decode(x.raw, np.ones_like(x.scales), x.dtype, d)
+        live = np.isfinite(k)
+        k[..., channels > 2.0 ** -4 * 30] = 0
+        enc = co.encode(np.where(live, k, 0), np.where(np.isfinite(v), v, 0), x.dtype)
+        x.raw[:, :, 0] = enc[:, :, 0]
+    check_attend(g, [300, 128], [min(rows, n) for n in (300, 128)], rows, 4, 2, d, 0, spoil=spoil, channels=channels, scale=1.0)
 
 
 def test_pages_of_very_different_scales():
