@@ -153,16 +153,23 @@ def _bytes(x, dtype):
 
 def attend(Q, k, v, there, kv, q, scale):
     """One request: Q [H, n, d]; k, v [Hkv, positions, d]; there [positions] (the position lies in a page);
-    the n newest of kv tokens.  64 bits; rows without a key give 0."""
+    the q newest of kv tokens.  64 bits; rows without a key, and rows q and up, give 0.  Also the weighted
+    sizes of the values and the largest sum |q k| scale of each row: (O, sizes [H, n, d], spread [H, n])."""
     H, n, d = Q.shape
     G = H // k.shape[0]
-    out = np.zeros((H, n, d))
-    for i in range(n):
-        seen = np.flatnonzero(there[:max(0, kv - q + i + 1)])
-        if not len(seen):
-            continue
-        for h in range(H):
-            s = (k[h // G][seen] @ Q[h, i]) * scale
-            p = np.exp(s - s.max())
-            out[h, i] = p @ v[h // G][seen] / p.sum()
-    return out
+    out, sizes, spread = np.zeros((H, n, d)), np.zeros((H, n, d)), np.zeros((H, n))
+    last = kv - q + np.arange(q)
+    seen = there[None, :] & (np.arange(len(there))[None, :] <= last[:, None])
+    rows = np.flatnonzero(seen.any(1))
+    if not len(rows):
+        return out, sizes, spread
+    seen = seen[rows]
+    for h in range(H):
+        kk, vv = k[h // G], v[h // G]
+        s = np.where(seen, (Q[h, rows] @ kk.T) * scale, -np.inf)
+        p = np.exp(s - s.max(1, keepdims=True))
+        p /= p.sum(1, keepdims=True)
+        out[h, rows] = p @ np.where(there[:, None], vv, 0)
+        sizes[h, rows] = p @ np.abs(np.where(there[:, None], vv, 0))
+        spread[h, rows] = np.where(seen, np.abs(Q[h, rows]) @ np.abs(kk).T, 0).max(1) * scale
+    return out, sizes, spread

@@ -291,25 +291,13 @@ def reference(x, b, Qv, kv, q, scale, tiles=False):
     tiles (many rows, e4m3, d 128 and 256): a query channel is two e4m3 numbers, off by 2^-22 of the
     largest of the 32 channels (in a row) that share a scale."""
     k, v, there = x.tokens(b, max(kv, 0))
-    O = co.attend(Qv, k, v, there, kv, q, scale)
-    H, G = Qv.shape[0], Qv.shape[0] // k.shape[0]
-    tol = np.zeros_like(O)
-    for i in range(q):
-        seen = np.flatnonzero(there[:max(0, kv - q + i + 1)])
-        if not len(seen):
-            continue
-        for h in range(H):
-            kk = k[h // G][seen]
-            s = (kk @ Qv[h, i]) * scale
-            p = np.exp(s - s.max())
-            p /= p.sum()
-            spread = (np.abs(kk) @ np.abs(Qv[h, i])).max() * scale
-            if tiles and x.d >= 128 and x.dtype == ugbs.E4M3:
-                m = np.repeat(np.abs(Qv[h, i]).reshape(x.d // 32, 32).max(1), 32)
-                spread += 2.0 ** -22 / (x.d + 3) * 2.0 ** 24 * (np.abs(kk) @ m).max() * scale
-            rel = 2.0 ** -8 + 2.02 * (x.d + 3) * 2.0 ** -24 * spread + (len(seen) + 64) * 2.0 ** -24
-            tol[h, i] = rel * (p @ np.abs(v[h // G][seen])) * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(O[h, i]) + 1e-30
-    return O, tol
+    O, sizes, spread = co.attend(Qv, k, v, there, kv, q, scale)
+    rel = 2.0 ** -8 + 2.02 * (x.d + 3) * 2.0 ** -24 * spread + (len(there) + 64) * 2.0 ** -24
+    if tiles and x.d >= 128 and x.dtype == ugbs.E4M3:
+        m = np.repeat(np.abs(Qv).reshape(Qv.shape[:2] + (x.d // 32, 32)).max(3), 32, axis=2)
+        big = np.abs(k).max(1, initial=0)                              # [Hkv, d], at least every key's
+        rel += 2.02 * 2.0 ** -22 * (m * np.repeat(big, Qv.shape[0] // k.shape[0], 0)[:, None]).sum(2) * scale
+    return O, rel[..., None] * sizes * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(O) + 1e-30
 
 
 def run_attend(c, x, Qb, kv, q, workspace=True, fill=7.0):
@@ -375,6 +363,19 @@ def test_several_tokens(rows, H, Hkv, d, dtype):
 def test_long_requests_are_split_and_joined(rows, H, Hkv, d, dtype, lens):
     g = np.random.default_rng(rows + H + d)
     check_attend(g, lens, [min(rows, n) for n in lens], rows, H, Hkv, d, dtype, max_pages=4096)
+
+
+@pytest.mark.parametrize("rows,H,Hkv,d,dtype,lens", [
+    (600, 16, 8, 64, 0, [9000]),                   # 152 tiles in three parts each: their rows joined four at a time
+    (300, 16, 8, 256, 1, [4000]),
+    (257, 16, 4, 128, 0, [3000, 257, 1000]),
+    (130, 12, 4, 256, 0, [5000, 64]),
+    (1000, 4, 1, 128, 0, [1000]),                  # a whole prompt
+    (515, 7, 1, 128, 1, [515, 600, 2000]),
+])
+def test_pieces_of_prompts(rows, H, Hkv, d, dtype, lens):
+    g = np.random.default_rng(rows + d)
+    check_attend(g, lens, [min(rows, n) for n in lens], rows, H, Hkv, d, dtype, max_pages=200)
 
 
 @pytest.mark.parametrize("B,rows,H,Hkv,d,dtype,longest", [
@@ -467,7 +468,8 @@ def test_two_calls_give_the_same_bits(rows, lens):
     assert torch.equal(a.view(torch.int16), b.view(torch.int16))
 
 
-def test_offsets_pass_32_bits():
+@pytest.mark.parametrize("rows", [1, 40])
+def test_offsets_pass_32_bits(rows):
     """A cache of more than 4 GiB, its last pages used."""
     d, Hkv, n_pages = 256, 8, 20000                # 5.2e9 bytes
     g = np.random.default_rng(14)
@@ -479,15 +481,16 @@ def test_offsets_pass_32_bits():
     cache[shift:] = dev(small.raw)
     scales[shift:] = dev(small.scales)
     table = np.where(small.table >= 0, small.table + shift, -1).astype(I32)
-    Qb, Qv = bf16(g.normal(0, 1, (2, 8, 1, d)))
-    c = ugbs.Cache.make(2, 8, Hkv, d, n_pages, small.max_pages)
-    O = torch.zeros((2, 8, 1, d), dtype=torch.bfloat16, device="cuda")
-    ugbs.ugbs_cache_attend(c, dev_bf16(Qb), cache, scales, dev(table), dev(np.array(lens, I32)), dev(np.array([1, 1], I32)), O,
+    Qb, Qv = bf16(g.normal(0, 1, (2, 8, rows, d)))
+    c = ugbs.Cache.make(2, 8, Hkv, d, n_pages, small.max_pages, rows=rows)
+    O = torch.zeros((2, 8, rows, d), dtype=torch.bfloat16, device="cuda")
+    ugbs.ugbs_cache_attend(c, dev_bf16(Qb), cache, scales, dev(table), dev(np.array(lens, I32)), dev(np.array([rows] * 2, I32)), O,
                            torch.empty(max(256, ugbs.ugbs_cache_workspace_bytes(c)), dtype=torch.uint8, device="cuda"))
     for b in range(2):
-        want, tol = reference(small, b, Qv[b], lens[b], 1, 1 / 16)
+        want, tol = reference(small, b, Qv[b], lens[b], rows, 1 / 16, rows > 16)
         assert (np.abs(bf16_to_f64(host_bits(O[b])) - want) <= tol).all()
     # a token stored into the last page, and loaded
+    c = ugbs.Cache.make(2, 8, Hkv, d, n_pages, small.max_pages)
     Kb, K = bf16(g.normal(0, 1, (2, Hkv, 1, d)))
     slots = np.array([[-1], [(n_pages - 1) * PAGE]], I32)
     ugbs.ugbs_cache_store(c, dev_bf16(Kb), dev_bf16(Kb), dev(slots), cache, scales)
@@ -609,6 +612,42 @@ def test_a_captured_step_replays_as_lengths_grow():
         assert torch.equal(sides[0][2].view(torch.int16), sides[1][2].view(torch.int16)), rep
         assert torch.equal(sides[0][1].table, sides[1][1].table) and torch.equal(sides[0][1].kv_lens, sides[1][1].kv_lens)
     assert sides[0][1].kv_lens.tolist() == [131] * 3
+
+
+def test_two_graphs_share_a_workspace():
+    """Captured calls of different sizes over one workspace, replayed in turn."""
+    g = np.random.default_rng(45)
+    x = Contents(g, [5000, 300], 2, 128, 0, max_pages=100)
+    cache, scales, table = x.device()
+    kv, q1 = dev(np.array([5000, 300], I32)), dev(np.array([1, 1], I32))
+    calls = []
+    for rows, n in ((1, 1), (40, 40)):
+        c = ugbs.Cache.make(2, 8, 2, 128, x.n_pages, 100, rows=rows)
+        Qb, Qv = bf16(g.normal(0, 1, (2, 8, rows, 128)))
+        calls.append((c, dev_bf16(Qb), Qv, dev(np.array([n, n], I32)), torch.zeros((2, 8, rows, 128), dtype=torch.bfloat16, device="cuda")))
+    ws = torch.empty(max(ugbs.ugbs_cache_workspace_bytes(y[0]) for y in calls), dtype=torch.uint8, device="cuda")
+    graphs = []
+    for c, Q, _, q, O in calls:
+        ugbs.ugbs_cache_attend(c, Q, cache, scales, table, kv, q, O, ws)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ugbs.ugbs_cache_attend(c, Q, cache, scales, table, kv, q, O, ws)
+        graphs.append(graph)
+    want = [O.clone() for *_, O in calls]
+    for rep in range(4):
+        for *_, O in calls:
+            O.fill_(3.0)
+        ws.fill_(rep)
+        for graph in graphs if rep % 2 else graphs[::-1]:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (c, _, Qv, q, O), w in zip(calls, want):
+            assert torch.equal(O.view(torch.int16), w.view(torch.int16)), rep
+    for c, _, Qv, q, O in calls:
+        for b in range(2):
+            ref, tol = reference(x, b, Qv[b], [5000, 300][b], c.rows, 1 / math.sqrt(128), c.rows > 1)
+            assert (np.abs(bf16_to_f64(host_bits(O[b])) - ref) <= tol).all()
 
 
 def test_streams_of_their_own():
