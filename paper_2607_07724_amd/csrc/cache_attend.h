@@ -5,9 +5,11 @@
 
 namespace ugbs {
 
-// Parts a call aims at, at most, and the pages of a part, at least: 128 KiB.
+// Parts a call aims at, at most, and the pages of a part, at least: 64 KiB, four pages
+// (one request of 4000 tokens at d 128: 11.3 us with 8 pages, 10.1 with 4; of 8000 at
+// d 256: 11.7 with 4, 12.4 with 2).
 constexpr int kTarget = 512;
-constexpr int min_pages(int d) { return 1024 / d; }
+constexpr int min_pages(int d) { return d == 64 ? 8 : 4; }
 // Parts of split tiles are at most twice W / X, X > W / kTarget, and a split tile has at least two.
 constexpr int kSlots = 2 * kTarget;
 
@@ -82,15 +84,16 @@ struct Part {
 
 // Pages per part, from the sums over the requests of tiles times pages and of tiles
 // (fp32, added in the same order wherever they are formed; + 1 covers the rounding, X
-// being at most 4096).  Each tile ends with a part that is not full, so kTarget is missed
-// by less than the tiles.  Where kTarget parts are what the chip holds at once (two a CU:
-// more than 16 rows) the tiles are taken off, down to half of it: 56 tiles as 560 parts
-// took two rounds, 264 us for 222.  With 16 rows four parts fit a CU, and the more the
-// better (32 ragged requests: 57 us, with half the parts 63).
+// being at most 4096).  Each tile ends with a part that is not full, half a part on average,
+// and kTarget parts are two a CU: half the tiles are taken off, so that few CUs get a
+// third (16 requests of up to 8000, 128 tiles: 36.0 -> 32.5 us; 32 ragged ones, 256 tiles: 57.1 ->
+// 54.6).  Where two are all that a CU holds at once (more than 16 rows) a third would be a
+// second round: there all tiles are taken off (56 tiles as 560 parts: 264 us for 222).
 template <int ROWS>
 __device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles) {
   if (!P.splits) return UGBS_MAX_BLOCKS;
-  const float aim = ROWS == 16 ? (float)kTarget : fmaxf((float)kTarget - tiles * (float)P.s.Hkv, 0.5f * kTarget);
+  const float off = (ROWS == 16 ? 0.5f : 1.0f) * tiles * (float)P.s.Hkv;
+  const float aim = fmaxf((float)kTarget - off, 0.5f * kTarget);
   const float x = work * (float)P.s.Hkv / aim;
   return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, P.min_pages) : UGBS_MAX_BLOCKS;
 }
@@ -158,7 +161,7 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
     work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
     tiles += (float)r[k].tiles;
   }
-  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, sum_wave(work), ROWS == 16 ? 0.f : sum_wave(tiles)));
+  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, sum_wave(work), sum_wave(tiles)));
   int before = 0, slots = 0;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {

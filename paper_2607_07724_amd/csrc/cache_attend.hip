@@ -14,7 +14,7 @@
 //
 // Work is split along the pages where there are few rows: with W the pages of
 // all tiles, a tile of n pages goes to ceil(n / X) workgroups, X just above W / 512
-// (at least 128 KiB), so that a long request among short ones does not hold
+// (at least 64 KiB), so that a long request among short ones does not hold
 // up the call.  The lengths are on the device; each wave forms the sums over
 // the requests for itself.  Parts leave their sums and maxima in the workspace,
 // and a second launch joins them, in the order of the pages.
