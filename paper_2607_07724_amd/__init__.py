@@ -650,7 +650,9 @@ class CacheStep:
         if stream is None:
             torch.add(self._after, 0, out=self._before)
         else:
-            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=self._after.device)):
+            dev = self._after.device
+            with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=dev) if stream
+                                   else torch.cuda.default_stream(dev)):
                 torch.add(self._after, 0, out=self._before)
         ugbs_cache_plan(c, self.ctx_lens, new_lens, self.free_pages, self.free_count, self.table, self.kv_lens,
                         self.q_lens, self.slots, self.free_left, stream)

@@ -26,12 +26,14 @@ namespace ugbs {
 namespace {
 
 // One part: RT tiles of 16 rows (all the rows of a kv head, so a byte is read by
-// one wave) against pages p0 .. p1 - 1.  The half pages (32
-// tokens) go round the waves; the waves' sums are joined in LDS at the end.  A
-// wave has one set of registers for a half page's bytes: the next keys are asked
-// for when the last product with these is issued, the next values likewise, so
-// one of the two is always on its way, and the registers leave room for more
-// waves, which hide the rest.
+// one wave) against pages p0 .. p1 - 1.  The half pages (32 tokens) go round the
+// waves; the waves' sums are joined in LDS at the end.  A wave has one set of
+// registers for a half page's bytes: the next keys are asked for when the last
+// product with these is issued, the next values likewise, so one of the two is
+// always on its way, and the registers leave room for more waves, which hide the
+// rest.  Bound by HBM: 32 ragged requests of up to 8K (32/8 heads, d 128, 276 MB)
+// 54.7 us with the join, 5.0 TB/s (a large copy reaches 4.97); one of 128K (28/4 heads,
+// 134 MB) 31.4 us, of which the join 4.
 template <int D, int DT, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendParams P) {
   constexpr int L = D / 32;                 // 16-byte loads of a lane: keys, and again values
@@ -200,7 +202,6 @@ bool may_split(const CacheShape& s) { return s.max_pages > min_pages(s.d); }
 template <int D, int DT, int RT>
 hipError_t attend_rows(const CacheAttendParams& P, hipStream_t stream) {
   constexpr int NW = 4, ROWS = 16 * RT;
-
   const int64_t units = tiles_bound(P.s, ROWS);
   launch_schedule<ROWS>(P, stream);
   cache_attend_rows_kernel<D, DT, RT, NW><<<(unsigned)(units + (P.splits ? kTarget : 0)), 64 * NW, 0, stream>>>(P);
@@ -247,8 +248,10 @@ hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uin
   CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, min_pages(s.d)};
   P.scale_log2 = s.scale * 1.4426950408889634f;
   P.splits = may_split(s);
-  P.part_o = static_cast<float*>(workspace);
-  P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)kSlots * tile_rows(s) * s.d);
+  if (P.splits) {
+    P.part_o = static_cast<float*>(workspace);
+    P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)kSlots * tile_rows(s) * s.d);
+  }
   if (s.B > kWaveBatch) {
     uint8_t* const at = static_cast<uint8_t*>(workspace) + align256(schedule_at(s));
     P.schedule.request = reinterpret_cast<int4*>(at);

@@ -674,6 +674,27 @@ def test_streams_of_their_own():
             assert (np.abs(bf16_to_f64(host_bits(O[b])) - want) <= tol).all()
 
 
+def test_a_step_on_streams_given_as_handles():
+    g = np.random.default_rng(55)
+    c = ugbs.Cache.make(2, 4, 2, 64, 20, 4)
+    Qb, Kb, Vb = (bf16(g.normal(0, 1, (2, h, 1, 64)))[0] for h in (4, 2, 2))
+    t = [dev_bf16(x) for x in (Qb, Kb, Vb)]
+    new = dev(np.array([1, 1], I32))
+    side = torch.cuda.Stream()
+    outs = []
+    for stream in (None, side.cuda_stream, 0):
+        cbufs, step = ugbs.CacheBuffers(c), ugbs.CacheStep(c)
+        O = torch.zeros_like(t[0])
+        torch.cuda.synchronize()
+        for _ in range(3):
+            step.plan(c, new, stream)
+            ugbs.cache_layer(c, *t, O, cbufs, step, stream)
+        torch.cuda.synchronize()
+        assert step.kv_lens.tolist() == [3, 3] and int(step.free_left.item()) == 18
+        outs.append(O)
+    assert all(torch.equal(outs[0].view(torch.int16), x.view(torch.int16)) for x in outs)
+
+
 def test_cached_prompt_through_the_sparse_prefill():
     """Loaded keys and values are bf16 tensors like any other: the prefill over them equals the prefill
     over the same numbers."""
