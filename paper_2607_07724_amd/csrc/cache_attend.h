@@ -430,7 +430,7 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
 template <int D, int ROWS, int JR>
 __global__ void __launch_bounds__(JR == 1 ? 256 : 512) cache_join_kernel(CacheAttendParams P, int row_groups, int items) {
   constexpr int kJoin = JR == 1 ? 256 : 512, kJoinRows = JR;
-  constexpr int CG = D / 4, GR = kJoin / kJoinRows / CG, kAhead = 8;
+  constexpr int CG = D / 4, GR = kJoin / kJoinRows / CG, kAhead = JR == 1 ? 16 : 8;
   constexpr int TR = kJoin / kJoinRows;     // threads of a row
   __shared__ float2 s_part[kJoinRows][kSlots / 2];   // maximum, then weight; sum
   __shared__ float2 s_ml[kJoin / 64];
@@ -455,10 +455,11 @@ __global__ void __launch_bounds__(JR == 1 ? 256 : 512) cache_join_kernel(CacheAt
       M = fmaxf(M, s_part[jr][v].x);
     }
     f32x4 ahead[kAhead];
+    const int most = __builtin_amdgcn_readfirstlane(u.splits);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       const int v = gr + k * GR;
-      ahead[k] = splits > 0 ? po[(size_t)min(v, splits - 1) * (ROWS * CG)] : f32x4{0.f, 0.f, 0.f, 0.f};
+      if (k * GR < most) ahead[k] = po[(size_t)min(v, max(splits, 1) - 1) * (ROWS * CG)];
     }
 #pragma unroll
     for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
