@@ -426,7 +426,8 @@ UGBS_API size_t ugbs_workspace_bytes(const ugbs_problem* p);
  * layer:
  *   cache  : [n_pages, H_kv, 2, 64 d] bytes, 16-byte aligned: per page of 64
  *            tokens and kv head the keys, then the values;
- *   scales : [n_pages, H_kv, 2] fp32, 8-byte aligned: their scales.
+ *   scales : [n_pages, H_kv, 2] fp32, 8-byte aligned: their scales, powers of
+ *            two as ugbs_cache_store writes them (others are not supported).
  * A byte stands for its number (e4m3: 4 exponent bits, bias 7, 3 fraction
  * bits, largest 448, no infinities; or a signed integer, -127..127) times the
  * scale.  Token t = 0..63 of a page, channel c:
@@ -525,7 +526,12 @@ UGBS_API int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float
  *   i and, for query head h and kv head h / (H / H_kv),
  *   O_i = sum_{j <= p_i} softmax_j(scale * q_i . k_j) v_j with the cached k, v:
  *   bf16 products, fp32 accumulation and softmax, probabilities rounded to bf16
- *   for the second product.  A row that sees no key (p_i < 0, or no page) gives 0.
+ *   for the second product.  With e4m3, d 128 or 256 and more than 32 (16 at d 256)
+ *   query rows to a kv head (rows H / H_kv), a query channel enters the first product as
+ *   two e4m3 numbers: exact but for what lies below 2^-22 of the largest of its 32
+ *   channels (32 j .. 32 j + 31).  A row that sees no key (p_i < 0, or no page)
+ *   gives 0.  Results do not depend on timing: equal calls on equal GPUs agree bit
+ *   for bit.
  *   Q, O      : [B, H, rows, d] bf16, 16-byte aligned.  Rows q_lens[b] and up are
  *               neither read nor written.
  *   kv_lens   : [B] int32 (taken as 0..64 max_pages).
