@@ -87,12 +87,12 @@ struct Part {
 // being at most 4096).  Each tile ends with a part that is not full, half a part on average,
 // and kTarget parts are two a CU: half the tiles are taken off, so that few CUs get a
 // third (16 requests of up to 8000, 128 tiles: 36.0 -> 32.5 us; 32 ragged ones, 256 tiles: 57.1 ->
-// 54.6).  Where two are all that a CU holds at once (more than 16 rows) a third would be a
-// second round: there all tiles are taken off (56 tiles as 560 parts: 264 us for 222).
+// 54.6).  At 64 rows two are all that a CU holds at once, and a third is a second round: there
+// three quarters of the tiles are taken off (56 tiles: as 560 parts 264 us, as 504 193).
 template <int ROWS>
 __device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles) {
   if (!P.splits) return UGBS_MAX_BLOCKS;
-  const float off = (ROWS == 16 ? 0.5f : 1.0f) * tiles * (float)P.s.Hkv;
+  const float off = (ROWS <= 32 ? 0.5f : 0.75f) * tiles * (float)P.s.Hkv;
   const float aim = fmaxf((float)kTarget - off, 0.5f * kTarget);
   const float x = work * (float)P.s.Hkv / aim;
   return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, P.min_pages) : UGBS_MAX_BLOCKS;
