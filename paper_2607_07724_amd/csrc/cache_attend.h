@@ -369,6 +369,12 @@ __device__ __forceinline__ uint2 live_bytes(int kv, int key0) {
   return make_uint2(keep[0], keep[1]);
 }
 
+__device__ __forceinline__ void store_row(const CacheAttendParams& P, const Part& u, int D, int at_row, int c, const f32x4& o, float inv) {
+  const int i = at_row / P.s.G, h = u.kvh * P.s.G + at_row % P.s.G;
+  *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * P.s.H + h) * P.s.rows + i) * D + c) =
+      make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+}
+
 // The waves' sums of a part, 16 rows at a time: O, or the part's slot.  seen: a
 // key of the row has been looked at.  s_o: [NW][16][D + 4] floats, s_ml: [NW][16 RT].
 template <int D, int RT, int NW>
@@ -409,10 +415,7 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
         for (int e = 0; e < 4; ++e) o[e] += a * ov[e];
       }
       if (u.splits == 1) {
-        const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
-        const float inv = reciprocal(M, l);
-        *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + c) =
-            make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
+        store_row(P, u, D, at_row, c, o, reciprocal(M, l));
       } else {
         const size_t slot = (size_t)u.slot + u.split;
         *reinterpret_cast<f32x4*>(P.part_o + (slot * ROWS + rr) * D + c) = o;
@@ -422,92 +425,129 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
   }
 }
 
-// Joins the parts of split tiles: D / 4 threads to a row and part, the parts of a row
-// round its threads; the first kAhead parts of a thread are on their way before the
-// weights are known.  Few rows in all (JR 1): a workgroup for each row that there could
-// be.  Many (JR 4): four rows of a tile at a time, by workgroups that go on to the next
-// four (a workgroup for each row took 16 us at 64 rows a tile where nothing was split).
-template <int D, int ROWS, int JR>
-__global__ void __launch_bounds__(JR == 1 ? 256 : 512) cache_join_kernel(CacheAttendParams P, int row_groups, int items) {
-  constexpr int kJoin = JR == 1 ? 256 : 512, kJoinRows = JR;
-  constexpr int CG = D / 4, GR = kJoin / kJoinRows / CG, kAhead = JR == 1 ? 16 : 8;
-  constexpr int TR = kJoin / kJoinRows;     // threads of a row
-  __shared__ float2 s_part[kJoinRows][kSlots / 2];   // maximum, then weight; sum
-  __shared__ float2 s_ml[kJoin / 64];
-  __shared__ f32x4 s_o[GR][kJoinRows][CG];
-  static_assert(TR % 64 == 0 && GR * CG == TR, "whole waves to a row");
-  const CacheShape& s = P.s;
-  const int tid = threadIdx.x, w = tid >> 6;
-  const int jr = tid / TR, tr = tid % TR, gr = tr / CG, c = tr % CG;
-  int item = blockIdx.x;
-  do {
-    Part u;
-    if (!find_part<ROWS, kJoinTiles>(P, JR == 1 ? item : item / row_groups, &u)) return;
-    const int rr = JR == 1 ? blockIdx.y : item % row_groups * kJoinRows + jr, at_row = u.tile * ROWS + rr;
-    const bool ok = at_row < u.q * s.G;
-    const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
-    const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
-    if (JR == 1 && !ok) return;            // the whole workgroup's row
-    const int splits = ok ? u.splits : 0;   // of this thread's row
-    float M = -__builtin_huge_valf();
-    for (int v = tr; v < splits; v += TR) {
-      s_part[jr][v] = ml[(size_t)v * ROWS];
-      M = fmaxf(M, s_part[jr][v].x);
+// Joins the parts of split tiles where few tiles can have many parts: a workgroup for
+// each row that there could be, D / 4 threads to a part, the parts round its threads; the
+// first kAhead parts of a thread are on their way before the weights are known.
+template <int D, int ROWS>
+__global__ void __launch_bounds__(256) cache_join_kernel(CacheAttendParams P) {
+  constexpr int CG = D / 4, GR = 256 / CG, kAhead = 16;
+  __shared__ float2 s_part[kSlots / 2];     // maximum, then weight; sum
+  __shared__ float2 s_ml[4];
+  __shared__ f32x4 s_o[GR][CG];
+  Part u;
+  if (!find_part<ROWS, kJoinTiles>(P, blockIdx.x, &u)) return;
+  const int tid = threadIdx.x, w = tid >> 6, rr = blockIdx.y, at_row = u.tile * ROWS + rr;
+  if (at_row >= u.q * P.s.G) return;
+  const int gr = tid / CG, c = tid % CG, splits = __builtin_amdgcn_readfirstlane(u.splits);
+  const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
+  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
+  float M = -__builtin_huge_valf();
+  for (int v = tid; v < splits; v += 256) {
+    s_part[v] = ml[(size_t)v * ROWS];
+    M = fmaxf(M, s_part[v].x);
+  }
+  f32x4 ahead[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (k * GR < splits) ahead[k] = po[(size_t)min(gr + k * GR, splits - 1) * (ROWS * CG)];
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
+  if ((tid & 63) == 0) s_ml[w].x = M;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < 4; ++v) M = fmaxf(M, s_ml[v].x);
+  float l = 0.f;
+  for (int v = tid; v < splits; v += 256) {
+    const float2 x = s_part[v];
+    // a part that saw none of the row's keys weighs nothing
+    const float a = x.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(x.x - M);
+    s_part[v].x = a;
+    if (a != 0.f) l += a * x.y;
+  }
+  l = sum_wave(l);
+  if ((tid & 63) == 0) s_ml[w].y = l;
+  __syncthreads();
+  l = 0.f;
+#pragma unroll
+  for (int v = 0; v < 4; ++v) l += s_ml[v].y;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto add = [&](int v, const f32x4& x) {
+    const float a = s_part[v].x;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] += a * x[e];
+  };
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (gr + k * GR < splits) add(gr + k * GR, ahead[k]);
+#pragma unroll 4
+  for (int v = gr + kAhead * GR; v < splits; v += GR) add(v, po[(size_t)v * (ROWS * CG)]);
+  s_o[gr][c] = o;
+  __syncthreads();
+  if (gr == 0) {
+#pragma unroll
+    for (int v = 1; v < GR; ++v)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] += s_o[v][c][e];
+    store_row(P, u, D, at_row, 4 * c, o, reciprocal(M, l));
+  }
+}
+
+// The same where many tiles have few parts each: 1024 / D rows of a tile a workgroup, D / 4
+// threads to a row, which take its parts eight at a time; nothing is shared.  (256 tiles
+// of 64 rows in two parts each: 25 us with the kernel above's way, 5 with this one.)
+template <int D, int ROWS>
+__global__ void __launch_bounds__(256) cache_join_rows_kernel(CacheAttendParams P) {
+  constexpr int CG = D / 4, kAhead = 8;
+  // one wave looks the tile up: where no tile is split, that is all that 4096 workgroups do
+  __shared__ Part s_u;
+  __shared__ int s_found;
+  if (threadIdx.x < 64) {
+    Part x;
+    const bool found = find_part<ROWS, kJoinTiles>(P, blockIdx.x, &x);
+    if (threadIdx.x == 0) {
+      s_found = found;
+      if (found) s_u = x;
     }
-    f32x4 ahead[kAhead];
-    const int most = __builtin_amdgcn_readfirstlane(u.splits);
+  }
+  __syncthreads();
+  if (!s_found) return;
+  const Part u = s_u;
+  const int tid = threadIdx.x, rr = blockIdx.y * (256 / CG) + tid / CG, c = tid % CG, at_row = u.tile * ROWS + rr;
+  if (rr >= ROWS || at_row >= u.q * P.s.G) return;
+  const int splits = __builtin_amdgcn_readfirstlane(u.splits);
+  const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
+  const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
+  float M = -__builtin_huge_valf(), l = 0.f;
+  f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int v = 0; v < splits; v += kAhead) {
+    float2 x[kAhead];
+    f32x4 y[kAhead];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int v = gr + k * GR;
-      if (k * GR < most) ahead[k] = po[(size_t)min(v, max(splits, 1) - 1) * (ROWS * CG)];
+      x[k] = make_float2(-__builtin_huge_valf(), 0.f);
+      if (v + k < splits) {
+        x[k] = ml[(size_t)(v + k) * ROWS];
+        y[k] = po[(size_t)(v + k) * (ROWS * CG)];
+      }
     }
+    float m = M;
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) M = fmaxf(M, __shfl_xor(M, o));
-    if ((tid & 63) == 0) s_ml[w].x = M;
-    __syncthreads();
+    for (int k = 0; k < kAhead; ++k) m = fmaxf(m, x[k].x);
+    const float alpha = M == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(M - m);
+    M = m;
+    l *= alpha;
 #pragma unroll
-    for (int v = 0; v < TR / 64; ++v) M = fmaxf(M, s_ml[jr * (TR / 64) + v].x);
-    float l = 0.f;
-    for (int v = tr; v < splits; v += TR) {
-      const float2 x = s_part[jr][v];
-      // a part that saw none of the row's keys weighs nothing
-      const float a = x.x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(x.x - M);
-      s_part[jr][v].x = a;
-      if (a != 0.f) l += a * x.y;
-    }
-    l = sum_wave(l);
-    if ((tid & 63) == 0) s_ml[w].y = l;
-    __syncthreads();
-    l = 0.f;
-#pragma unroll
-    for (int v = 0; v < TR / 64; ++v) l += s_ml[jr * (TR / 64) + v].y;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto add = [&](int v, const f32x4& x) {
-      const float a = s_part[jr][v].x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] += a * x[e];
-    };
+    for (int e = 0; e < 4; ++e) o[e] *= alpha;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k)
-      if (gr + k * GR < splits) add(gr + k * GR, ahead[k]);
-#pragma unroll 4
-    for (int v = gr + kAhead * GR; v < splits; v += GR) add(v, po[(size_t)v * (ROWS * CG)]);
-    s_o[gr][jr][c] = o;
-    __syncthreads();
-    if (gr == 0 && ok) {
+      if (v + k < splits && x[k].x != -__builtin_huge_valf()) {   // else the part saw none of the row's keys
+        const float a = __builtin_amdgcn_exp2f(x[k].x - m);
+        l += a * x[k].y;
 #pragma unroll
-      for (int v = 1; v < GR; ++v)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += s_o[v][jr][c][e];
-      const float inv = reciprocal(M, l);
-      const int i = at_row / s.G, h = u.kvh * s.G + at_row % s.G;
-      *reinterpret_cast<uint2*>(P.O + (((size_t)u.b * s.H + h) * s.rows + i) * D + 4 * c) =
-          make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
-    }
-    if (JR == 1) return;
-    __syncthreads();                        // the next rows use the same LDS
-    item += gridDim.x;
-  } while (item < items);
+        for (int e = 0; e < 4; ++e) o[e] += a * y[k][e];
+      }
+  }
+  store_row(P, u, D, at_row, 4 * c, o, reciprocal(M, l));
 }
 
 inline int64_t tiles_bound(const CacheShape& s, int rows_of_a_tile) {
@@ -531,11 +571,12 @@ void launch_join(const CacheAttendParams& P, hipStream_t stream) {
   const int64_t all_rows = (int64_t)P.s.rows * P.s.G, all_tiles = tiles_bound(P.s, ROWS);
   const int rows = (int)(all_rows < ROWS ? all_rows : ROWS);             // of a tile
   const int tiles = (int)(all_tiles < kTarget ? all_tiles : kTarget);    // at most kTarget are split
-  if (tiles * rows <= 8192) {
-    cache_join_kernel<D, ROWS, 1><<<dim3(tiles, rows), 256, 0, stream>>>(P, 0, 0);
+  // from 64 tiles on they have at most kSlots / 64 = 16 parts on average
+  if (tiles < 64) {
+    cache_join_kernel<D, ROWS><<<dim3(tiles, rows), 256, 0, stream>>>(P);
   } else {
-    const int groups = (rows + 3) / 4;
-    cache_join_kernel<D, ROWS, 4><<<512, 512, 0, stream>>>(P, groups, tiles * groups);
+    constexpr int per = 1024 / D;
+    cache_join_rows_kernel<D, ROWS><<<dim3(tiles, (rows + per - 1) / per), 256, 0, stream>>>(P);
   }
 }
 
