@@ -375,13 +375,16 @@ __device__ __forceinline__ void store_row(const CacheAttendParams& P, const Part
       make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
 }
 
-// The waves' sums of a part, 16 rows at a time: O, or the part's slot.  seen: a
-// key of the row has been looked at.  s_o: [NW][16][D + 4] floats, s_ml: [NW][16 RT].
+// The waves' sums of a part: O, or the part's slot.  seen: a key of the row has been
+// looked at.  Each wave brings its own to the rows' maxima first (and, where the part is
+// the whole, divides by the sums), so what is left are plain sums, 16 rows at a time, of
+// values that lie in LDS as the lanes hold them.  s_o: NW D 16 floats, 16-byte aligned, may be
+// what the waves still use on entry; s_ml: [NW][16 RT], may not.
 template <int D, int RT, int NW>
 __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Part& u, float* s_o, float2* s_ml,
-                                            const f32x4 (&acc)[RT][D / 16], const float (&m_run)[RT],
-                                            const float (&l_run)[RT], const bool (&seen)[RT]) {
-  constexpr int ROWS = 16 * RT, CG = D / 4, W = D + 4;   // 4 channels a thread
+                                            f32x4 (&acc)[RT][D / 16], const float (&m_run)[RT], const float (&l_run)[RT],
+                                            const bool (&seen)[RT]) {
+  constexpr int ROWS = 16 * RT, DT = D / 16;
   const CacheShape& s = P.s;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4, c16 = lane & 15;
 #pragma unroll
@@ -389,37 +392,45 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
     const float l = sum_groups(l_run[rt]);
     if (g == 0) s_ml[w * ROWS + 16 * rt + c16] = make_float2(seen[rt] ? m_run[rt] : -__builtin_huge_valf(), l);
   }
+  __syncthreads();
+  const size_t slot = (size_t)u.slot + u.split;
+  f32x4* const so = reinterpret_cast<f32x4*>(s_o);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
+    const int rr = 16 * rt + c16;
+    float M = -__builtin_huge_valf(), l = 0.f, mine = 0.f;
+    float2 ml[NW];
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      ml[v] = s_ml[v * ROWS + rr];
+      M = fmaxf(M, ml[v].x);
+    }
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float a = ml[v].x == -__builtin_huge_valf() ? 0.f : __builtin_amdgcn_exp2f(ml[v].x - M);
+      l += a * ml[v].y;
+      if (v == w) mine = a;
+    }
+    if (u.splits == 1) mine *= reciprocal(M, l);
+    else if (w == 0 && g == 0) P.part_ml[slot * ROWS + rr] = make_float2(M, l);
     if (rt > 0) __syncthreads();
 #pragma unroll
-    for (int dt = 0; dt < D / 16; ++dt) *reinterpret_cast<f32x4*>(s_o + (w * 16 + c16) * W + 16 * dt + 4 * g) = acc[rt][dt];
+    for (int dt = 0; dt < DT; ++dt) {
+      f32x4 x = acc[rt][dt];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] *= mine;
+      so[(w * DT + dt) * 64 + lane] = x;
+    }
     __syncthreads();
-    for (int k = tid; k < 16 * CG; k += 64 * NW) {
-      const int r16 = k / CG, c = 4 * (k % CG), rr = 16 * rt + r16;
-      const int at_row = u.tile * ROWS + rr;
-      if (at_row >= u.q * s.G) continue;
-      float M = -__builtin_huge_valf();
 #pragma unroll
-      for (int v = 0; v < NW; ++v) M = fmaxf(M, s_ml[v * ROWS + rr].x);
-      float l = 0.f;
-      f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < DT / NW; ++k) {
+      const int dt = k * NW + w, at_row = u.tile * ROWS + rr, c = 16 * dt + 4 * g;
+      if (at_row < u.q * s.G) {
+        f32x4 o = so[dt * 64 + lane];
 #pragma unroll
-      for (int v = 0; v < NW; ++v) {
-        const float2 ml = s_ml[v * ROWS + rr];
-        if (ml.x == -__builtin_huge_valf()) continue;     // this wave saw none of the row's keys
-        const float a = __builtin_amdgcn_exp2f(ml.x - M);
-        l += a * ml.y;
-        const f32x4 ov = *reinterpret_cast<const f32x4*>(s_o + (v * 16 + r16) * W + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += a * ov[e];
-      }
-      if (u.splits == 1) {
-        store_row(P, u, D, at_row, c, o, reciprocal(M, l));
-      } else {
-        const size_t slot = (size_t)u.slot + u.split;
-        *reinterpret_cast<f32x4*>(P.part_o + (slot * ROWS + rr) * D + c) = o;
-        if (c == 0) P.part_ml[slot * ROWS + rr] = make_float2(M, l);
+        for (int v = 1; v < NW; ++v) o += so[(v * DT + dt) * 64 + lane];
+        if (u.splits == 1) store_row(P, u, D, at_row, c, o, 1.0f);
+        else *reinterpret_cast<f32x4*>(P.part_o + (slot * ROWS + rr) * D + c) = o;
       }
     }
   }

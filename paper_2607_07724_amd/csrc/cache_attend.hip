@@ -38,7 +38,7 @@ template <int D, int DT, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendParams P) {
   constexpr int L = D / 32;                 // 16-byte loads of a lane: keys, and again values
   constexpr int ROWS = 16 * RT;
-  __shared__ __align__(16) float s_o[NW][16][D + 4];
+  __shared__ __align__(16) float s_o[NW * 16 * D];
   __shared__ float2 s_ml[NW][ROWS];
   const CacheShape& s = P.s;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c16 = lane & 15;
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   bool seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = key_first <= last[rt];
-  finish_part<D, RT, NW>(P, u, &s_o[0][0][0], &s_ml[0][0], acc, m_run, l_run, seen);
+  finish_part<D, RT, NW>(P, u, s_o, &s_ml[0][0], acc, m_run, l_run, seen);
 }
 
 bool may_split(const CacheShape& s) { return s.max_pages > min_pages(s.d); }

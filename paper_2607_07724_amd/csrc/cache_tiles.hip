@@ -110,8 +110,8 @@ cache_tiles_kernel(CacheAttendParams P) {
   constexpr int ROWS = 16 * RT;
   constexpr bool F8 = DT == UGBS_E4M3 && D >= 128;
   constexpr int kTile = 32 * D;             // bytes of a half page's keys (values)
-  constexpr int kAll = NW * 2 * kTile, kOut = NW * 16 * (D + 4) * 4;
-  __shared__ __align__(16) uint8_t s_mem[kAll > kOut ? kAll : kOut];
+  __shared__ __align__(16) uint8_t s_mem[NW * 2 * kTile];   // at the end: 16 rows' sums of every wave
+  static_assert(sizeof(float) * NW * 16 * D <= NW * 2 * kTile, "they fit");
   __shared__ float2 s_ml[NW * ROWS];
   __shared__ __align__(16) uint4 s_q[QR < RT ? (RT - QR) * 2 * E * 64 : 1];   // rows of tiles QR.., as operands
   __shared__ uint32_t s_qs[F8 ? RT * (E / 2) * 64 : 1];                                     // their scales
@@ -391,7 +391,6 @@ cache_tiles_kernel(CacheAttendParams P) {
   bool seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = key_first <= last(rt);
-  __syncthreads();                                       // the waves' tiles make room for the sums
   finish_part<D, RT, NW>(P, u, reinterpret_cast<float*>(s_mem), s_ml, acc, m_run, l_run, seen);
 }
 
