@@ -95,7 +95,9 @@ __device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float 
   const float off = (ROWS <= 32 ? 0.5f : 0.75f) * tiles * (float)P.s.Hkv;
   const float aim = fmaxf((float)kTarget - off, 0.5f * kTarget);
   const float x = work * (float)P.s.Hkv / aim;
-  return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, P.min_pages) : UGBS_MAX_BLOCKS;
+  // (256 tiles fill the chip: 512 tokens attending to themselves 26 us split, 20 whole)
+  const int least = tiles * (float)P.s.Hkv < 0.5f * kTarget ? P.min_pages : 2 * P.min_pages;
+  return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, least) : UGBS_MAX_BLOCKS;
 }
 __device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.pages > per ? (r.pages + per - 1) / per : 1; }
 
