@@ -12,6 +12,9 @@ constexpr int kTarget = 512;
 constexpr int min_pages(int d) { return d == 64 ? 8 : 4; }
 // Parts of split tiles are at most twice W / X, X > W / kTarget, and a split tile has at least two.
 constexpr int kSlots = 2 * kTarget;
+// A tile with more parts than kLongParts is long: joined by a workgroup for each row
+// (of 64 rows: for every fourth at least), also among many tiles.
+constexpr int kLongParts = 32, kLongTiles = kSlots / (kLongParts + 1);
 
 // Where the parts lie, of batches of more than kWaveBatch requests: formed once by
 // cache_schedule_kernel, in the workspace.  Up to kWaveBatch every wave forms it for itself
@@ -21,6 +24,7 @@ struct Schedule {
   int4* request;      // [B]: parts before, parts of a tile, slots before, split tiles before
   int32_t* part;      // [tiles + kTarget]: the request, -1 behind the last part
   int32_t* join;      // [kTarget]: the same for the split tiles
+  int2* long_tile;    // [kLongTiles]: request (-1 behind the last), which of its tiles
 };
 
 struct CacheAttendParams {
@@ -101,12 +105,13 @@ __device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float 
 }
 __device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.pages > per ? (r.pages + per - 1) / per : 1; }
 
-// Part number pos of the call (kJoinTiles: tile number pos among the split ones).
+// Part number pos of the call (kJoinTiles: tile number pos among the split ones,
+// kLongTilesOnly: among the long ones).
 // The parts of a request follow each other.  kParts: kv head, tile, part.  kGroups:
 // tiles that read the same pages (kv head, part) on one XCD, one after another, so
 // that its L2 serves all but the first: workgroup j runs on XCD j mod 8, so groups
 // are dealt out 8 at a time, those that are left over in a row.  Uniform over the wave.
-enum Order { kParts, kGroups, kJoinTiles };
+enum Order { kParts, kGroups, kJoinTiles, kLongTilesOnly };
 template <Order ORDER>
 __device__ __forceinline__ void locate(const CacheAttendParams& P, int at, int tiles, int slots_before, Part* out) {
   out->split = 0;
@@ -138,8 +143,9 @@ template <int ROWS, Order ORDER>
 __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
   const int lane = threadIdx.x & 63, B = P.s.B, Hkv = P.s.Hkv;
   if (B > kWaveBatch) {
-    if (ORDER == kJoinTiles && pos >= kTarget) return false;
-    const int b = __builtin_amdgcn_readfirstlane((ORDER == kJoinTiles ? P.schedule.join : P.schedule.part)[pos]);
+    if ((ORDER == kJoinTiles && pos >= kTarget) || (ORDER == kLongTilesOnly && pos >= kLongTiles)) return false;
+    const int b = __builtin_amdgcn_readfirstlane(ORDER == kLongTilesOnly ? P.schedule.long_tile[pos].x
+                                                                         : (ORDER == kJoinTiles ? P.schedule.join : P.schedule.part)[pos]);
     if (b < 0) return false;
     const int4 x = P.schedule.request[b];
     const Lengths r = lengths_of<ROWS>(P, b);
@@ -147,7 +153,7 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
     out->q = r.q;
     out->kv = r.kv;
     out->splits = x.y;
-    locate<ORDER>(P, pos - (ORDER == kJoinTiles ? x.w : x.x), r.tiles, x.z, out);
+    locate<ORDER>(P, ORDER == kLongTilesOnly ? P.schedule.long_tile[pos].y : pos - (ORDER == kJoinTiles ? x.w : x.x), r.tiles, x.z, out);
     return true;
   }
   constexpr int NC = kWaveBatch / 64;
@@ -170,7 +176,9 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
     if (64 * k >= B) return false;
     const int splits = splits_of(r[k], per), units = r[k].tiles * Hkv;
     const int used = splits > 1 ? units * splits : 0;
-    const int mine = ORDER == kJoinTiles ? (splits > 1 ? units : 0) : units * splits;
+    const int mine = ORDER == kJoinTiles       ? (splits > 1 ? units : 0)
+                     : ORDER == kLongTilesOnly ? (splits > kLongParts ? units : 0)
+                                               : units * splits;
     const int upto = before + scan_add(mine), slots_upto = slots + scan_add(used);
     const unsigned long long found = __ballot(pos >= upto - mine && pos < upto);
     if (found) {
@@ -196,7 +204,7 @@ template <int ROWS>
 __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheAttendParams P, int entries) {
   constexpr int PER = UGBS_MAX_REQUESTS / kScheduleThreads, NW = kScheduleThreads / 64;
   __shared__ int s_parts[UGBS_MAX_REQUESTS], s_joins[UGBS_MAX_REQUESTS];
-  __shared__ int s_wave[3][NW];
+  __shared__ int s_wave[4][NW];
   __shared__ float2 s_work[NW];
   const int tid = threadIdx.x, w = tid >> 6, B = P.s.B, Hkv = P.s.Hkv;
   Lengths r[PER];
@@ -223,7 +231,7 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
     tiles += s_work[v].y;
   }
   const int per = pages_per_part<ROWS>(P, work, tiles);
-  int n[3] = {0, 0, 0};                     // parts, slots, split tiles
+  int n[4] = {0, 0, 0, 0};                  // parts, slots, split tiles, long tiles
   int splits[PER];
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
@@ -234,20 +242,21 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
       n[1] += units * splits[k];
       n[2] += units;
     }
+    if (splits[k] > kLongParts) n[3] += units;
   }
-  int at[3];
+  int at[4];
 #pragma unroll
-  for (int x = 0; x < 3; ++x) {
+  for (int x = 0; x < 4; ++x) {
     const int in = scan_add(n[x]);
     at[x] = in - n[x];
     if ((tid & 63) == 63) s_wave[x][w] = in;
   }
   __syncthreads();
-  int total[3] = {0, 0, 0};
+  int total[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int v = 0; v < NW; ++v)
 #pragma unroll
-    for (int x = 0; x < 3; ++x) {
+    for (int x = 0; x < 4; ++x) {
       if (v < w) at[x] += s_wave[x][v];
       total[x] += s_wave[x][v];
     }
@@ -264,6 +273,8 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
         at[1] += units * splits[k];
         at[2] += units;
       }
+      if (blockIdx.x == 0 && splits[k] > kLongParts)
+        for (int i = 0; i < units; ++i) P.schedule.long_tile[at[3]++] = make_int2(b, i);
     }
   }
   __syncthreads();
@@ -279,6 +290,7 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
   };
   for (int i = blockIdx.x * kScheduleThreads + tid; i < entries; i += gridDim.x * kScheduleThreads)
     P.schedule.part[i] = i < total[0] ? request_at(s_parts, i) : -1;
+  if (blockIdx.x == 0 && tid >= total[3] && tid < kLongTiles) P.schedule.long_tile[tid] = make_int2(-1, 0);
   if (blockIdx.x == 0 && tid < kTarget) P.schedule.join[tid] = tid < total[2] ? request_at(s_joins, tid) : -1;
 }
 
@@ -438,18 +450,16 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
   }
 }
 
-// Joins the parts of split tiles where few tiles can have many parts: a workgroup for
-// each row that there could be, D / 4 threads to a part, the parts round its threads; the
-// first kAhead parts of a thread are on their way before the weights are known.
+// Joins the parts of row rr of a split tile: the work of a workgroup, D / 4 threads to a
+// part, the parts round its threads; the first kAhead parts of a thread are on their way before
+// the weights are known.  May be called again for another row without a barrier between.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(256) cache_join_kernel(CacheAttendParams P) {
+__device__ __forceinline__ void join_row(const CacheAttendParams& P, const Part& u, int rr) {
   constexpr int CG = D / 4, GR = 256 / CG, kAhead = 16;
   __shared__ float2 s_part[kSlots / 2];     // maximum, then weight; sum
   __shared__ float2 s_ml[4];
   __shared__ f32x4 s_o[GR][CG];
-  Part u;
-  if (!find_part<ROWS, kJoinTiles>(P, blockIdx.x, &u)) return;
-  const int tid = threadIdx.x, w = tid >> 6, rr = blockIdx.y, at_row = u.tile * ROWS + rr;
+  const int tid = threadIdx.x, w = tid >> 6, at_row = u.tile * ROWS + rr;
   if (at_row >= u.q * P.s.G) return;
   const int gr = tid / CG, c = tid % CG, splits = __builtin_amdgcn_readfirstlane(u.splits);
   const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
@@ -505,18 +515,31 @@ __global__ void __launch_bounds__(256) cache_join_kernel(CacheAttendParams P) {
   }
 }
 
-// The same where many tiles have few parts each: 1024 / D rows of a tile a workgroup, D / 4
-// threads to a row, which take its parts eight at a time; nothing is shared.  (256 tiles
-// of 64 rows in two parts each: 25 us with the kernel above's way, 5 with this one.)
+// Few tiles, which can have many parts: a workgroup for each row that there could be.
 template <int D, int ROWS>
-__global__ void __launch_bounds__(256) cache_join_rows_kernel(CacheAttendParams P) {
+__global__ void __launch_bounds__(256) cache_join_kernel(CacheAttendParams P) {
+  Part u;
+  if (find_part<ROWS, kJoinTiles>(P, blockIdx.x, &u)) join_row<D, ROWS>(P, u, blockIdx.y);
+}
+
+// Many tiles, most of which have few parts: 1024 / D rows of a tile a workgroup, D / 4
+// threads to a row, which take its parts eight at a time; nothing is shared.  (256 tiles
+// of 64 rows in two parts each: 25 us with the kernel above, 5 with this one.)  LONG:
+// behind the workgroups of `tiles` tiles come those of the long ones, `each` times as many
+// a tile (one request of 200K tokens among 63 of 100, 8/1 heads: 95 us without them, 21 with; they
+// cost up to 3 us where no tile is long).
+template <int D, int ROWS, bool LONG>
+__global__ void __launch_bounds__(256) cache_join_rows_kernel(CacheAttendParams P, int tiles, int each) {
   constexpr int CG = D / 4, kAhead = 8;
   // one wave looks the tile up: where no tile is split, that is all that 4096 workgroups do
   __shared__ Part s_u;
   __shared__ int s_found;
+  const int past = LONG ? (int)blockIdx.x - tiles : -1;
   if (threadIdx.x < 64) {
     Part x;
-    const bool found = find_part<ROWS, kJoinTiles>(P, blockIdx.x, &x);
+    bool found;
+    if constexpr (LONG) found = past < 0 ? find_part<ROWS, kJoinTiles>(P, blockIdx.x, &x) : find_part<ROWS, kLongTilesOnly>(P, past / each, &x);
+    else found = find_part<ROWS, kJoinTiles>(P, blockIdx.x, &x);
     if (threadIdx.x == 0) {
       s_found = found;
       if (found) s_u = x;
@@ -525,9 +548,15 @@ __global__ void __launch_bounds__(256) cache_join_rows_kernel(CacheAttendParams 
   __syncthreads();
   if (!s_found) return;
   const Part u = s_u;
+  if constexpr (LONG)
+    if (past >= 0) {
+      for (int rr = past % each * gridDim.y + blockIdx.y; rr < ROWS; rr += each * gridDim.y) join_row<D, ROWS>(P, u, rr);
+      return;
+    }
+  const int splits = __builtin_amdgcn_readfirstlane(u.splits);
+  if (LONG && splits > kLongParts) return;
   const int tid = threadIdx.x, rr = blockIdx.y * (256 / CG) + tid / CG, c = tid % CG, at_row = u.tile * ROWS + rr;
   if (rr >= ROWS || at_row >= u.q * P.s.G) return;
-  const int splits = __builtin_amdgcn_readfirstlane(u.splits);
   const float2* const ml = P.part_ml + (size_t)u.slot * ROWS + rr;
   const f32x4* const po = reinterpret_cast<const f32x4*>(P.part_o + ((size_t)u.slot * ROWS + rr) * D) + c;
   float M = -__builtin_huge_valf(), l = 0.f;
@@ -584,12 +613,18 @@ void launch_join(const CacheAttendParams& P, hipStream_t stream) {
   const int64_t all_rows = (int64_t)P.s.rows * P.s.G, all_tiles = tiles_bound(P.s, ROWS);
   const int rows = (int)(all_rows < ROWS ? all_rows : ROWS);             // of a tile
   const int tiles = (int)(all_tiles < kTarget ? all_tiles : kTarget);    // at most kTarget are split
-  // from 64 tiles on they have at most kSlots / 64 = 16 parts on average
+  // from 64 tiles on most have few parts: at most 16 (kSlots / 64) on average, if all are split
   if (tiles < 64) {
     cache_join_kernel<D, ROWS><<<dim3(tiles, rows), 256, 0, stream>>>(P);
   } else {
     constexpr int per = 1024 / D;
-    cache_join_rows_kernel<D, ROWS><<<dim3(tiles, (rows + per - 1) / per), 256, 0, stream>>>(P);
+    const int groups = (rows + per - 1) / per;
+    const int each = ((rows < 16 ? rows : 16) + groups - 1) / groups;
+    // (a part has min_pages at least)
+    if (P.s.max_pages > kLongParts * P.min_pages)
+      cache_join_rows_kernel<D, ROWS, true><<<dim3(tiles + kLongTiles * each, groups), 256, 0, stream>>>(P, tiles, each);
+    else
+      cache_join_rows_kernel<D, ROWS, false><<<dim3(tiles, groups), 256, 0, stream>>>(P, tiles, 0);
   }
 }
 

@@ -238,7 +238,7 @@ size_t cache_attend_workspace(const CacheShape& s) {
   size_t n = schedule_at(s);
   if (s.B > kWaveBatch)
     n = align256(n) + align256(s.B * sizeof(int4)) + align256(schedule_entries(s, tile_rows(s)) * sizeof(int32_t)) +
-        kTarget * sizeof(int32_t);
+        kTarget * sizeof(int32_t) + kLongTiles * sizeof(int2);
   return n;
 }
 
@@ -258,6 +258,7 @@ hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uin
     P.schedule.part = reinterpret_cast<int32_t*>(at + align256(s.B * sizeof(int4)));
     P.schedule.join = reinterpret_cast<int32_t*>(reinterpret_cast<uint8_t*>(P.schedule.part) +
                                                  align256(schedule_entries(s, tile_rows(s)) * sizeof(int32_t)));
+    P.schedule.long_tile = reinterpret_cast<int2*>(P.schedule.join + kTarget);
   }
   const bool f8 = s.dtype == UGBS_E4M3;
   if (s.d == 64) return f8 ? attend<64, UGBS_E4M3>(P, stream) : attend<64, UGBS_INT8>(P, stream);

@@ -366,7 +366,7 @@ def test_long_requests_are_split_and_joined(rows, H, Hkv, d, dtype, lens):
 
 
 @pytest.mark.parametrize("rows,H,Hkv,d,dtype,lens", [
-    (600, 16, 8, 64, 0, [9000]),                   # 152 tiles in three parts each: their rows joined four at a time
+    (600, 16, 8, 64, 0, [9000]),                   # 152 tiles in three parts each
     (300, 16, 8, 256, 1, [4000]),
     (257, 16, 4, 128, 0, [3000, 257, 1000]),
     (130, 12, 4, 256, 0, [5000, 64]),
@@ -388,6 +388,18 @@ def test_many_requests_among_them_a_long_one(B, rows, H, Hkv, d, dtype, longest)
     q = [int(min(n, m)) for n, m in zip(lens, g.integers(0, rows + 1, B))]
     q[B // 2 + 7] = min(rows, longest)
     check_attend(g, lens, q, rows, H, Hkv, d, dtype, max_pages=200)
+
+
+@pytest.mark.parametrize("B,rows,H,Hkv,d,dtype,longest", [
+    (64, 1, 4, 1, 128, 0, 30000), (300, 1, 4, 1, 128, 1, 40000), (64, 3, 8, 1, 256, 0, 20000), (70, 9, 4, 1, 64, 0, 40000),
+    (300, 20, 4, 1, 128, 0, 30000), (100, 2, 8, 2, 128, 0, 33333), (260, 5, 4, 2, 256, 1, 50000)])
+def test_tiles_of_many_parts_among_many_tiles(B, rows, H, Hkv, d, dtype, longest):
+    g = np.random.default_rng(B + rows + d)
+    lens = [int(n) for n in g.integers(0, 70, B)]
+    lens[B // 3], lens[B - 1] = longest, 3000      # above 32 parts a tile, and a few
+    q = [int(min(n, m)) for n, m in zip(lens, g.integers(0, rows + 1, B))]
+    q[B // 3] = q[B - 1] = rows
+    check_attend(g, lens, q, rows, H, Hkv, d, dtype, max_pages=1000)
 
 
 def test_sharp_and_flat_softmax():
