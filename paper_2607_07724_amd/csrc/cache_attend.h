@@ -86,22 +86,28 @@ struct Part {
   int b, kvh, tile, split, splits, slot, q, kv;   // slot: of the tile's first part
 };
 
-// Pages per part, from the sums over the requests of tiles times pages and of tiles
-// (fp32, added in the same order wherever they are formed; + 1 covers the rounding, X
-// being at most 4096).  Each tile ends with a part that is not full, half a part on average,
-// and kTarget parts are two a CU: half the tiles are taken off, so that few CUs get a
+// Pages per part, from the sums over the requests of tiles times pages, of tiles and of
+// wide tiles (fp32, added in the same order wherever they are formed; + 1 covers the
+// rounding, X being at most 4096).  Each tile ends with a part that is not full, half a part on
+// average, and kTarget parts are two a CU: half the tiles are taken off, so that few CUs get a
 // third (16 requests of up to 8000, 128 tiles: 36.0 -> 32.5 us; 32 ragged ones, 256 tiles: 57.1 ->
 // 54.6).  At 64 rows two are all that a CU holds at once, and a third is a second round: there
-// three quarters of the tiles are taken off (56 tiles: as 560 parts 264 us, as 504 193).
+// three quarters of the tiles are taken off (56 tiles: as 560 parts 264 us, as 504 193).  Tiles
+// of a few pages among long ones end no part that matters and are not counted (one request
+// of 100K among 3 of 100, 64 rows of 64/16 heads, d 64: 220 -> 156 us).
 template <int ROWS>
-__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles) {
+__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles, float wide) {
   if (!P.splits) return UGBS_MAX_BLOCKS;
-  const float off = (ROWS <= 32 ? 0.5f : 0.75f) * tiles * (float)P.s.Hkv;
+  const float off = (ROWS <= 32 ? 0.5f : 0.75f) * wide * (float)P.s.Hkv;
   const float aim = fmaxf((float)kTarget - off, 0.5f * kTarget);
   const float x = work * (float)P.s.Hkv / aim;
   // (256 tiles fill the chip: 512 tokens attending to themselves 26 us split, 20 whole)
   const int least = tiles * (float)P.s.Hkv < 0.5f * kTarget ? P.min_pages : 2 * P.min_pages;
   return x < (float)UGBS_MAX_BLOCKS ? max((int)x + 1, least) : UGBS_MAX_BLOCKS;
+}
+// Wide: of at least a quarter of work / kTarget pages.
+__device__ __forceinline__ bool is_wide(const CacheAttendParams& P, const Lengths& r, float work) {
+  return (float)r.pages * (4 * kTarget) > work * (float)P.s.Hkv;
 }
 __device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.pages > per ? (r.pages + per - 1) / per : 1; }
 
@@ -169,7 +175,12 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
     work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
     tiles += (float)r[k].tiles;
   }
-  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, sum_wave(work), sum_wave(tiles)));
+  work = sum_wave(work);
+  float wide = 0.f;
+#pragma unroll
+  for (int k = 0; k < NC; ++k)
+    if (is_wide(P, r[k], work)) wide += (float)r[k].tiles;
+  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, work, sum_wave(tiles), sum_wave(wide)));
   int before = 0, slots = 0;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
@@ -206,6 +217,7 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
   __shared__ int s_parts[UGBS_MAX_REQUESTS], s_joins[UGBS_MAX_REQUESTS];
   __shared__ int s_wave[4][NW];
   __shared__ float2 s_work[NW];
+  __shared__ float s_wide[NW];
   const int tid = threadIdx.x, w = tid >> 6, B = P.s.B, Hkv = P.s.Hkv;
   Lengths r[PER];
   float work = 0.f, tiles = 0.f;
@@ -230,7 +242,17 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
     work += s_work[v].x;
     tiles += s_work[v].y;
   }
-  const int per = pages_per_part<ROWS>(P, work, tiles);
+  float wide = 0.f;
+#pragma unroll
+  for (int k = 0; k < PER; ++k)
+    if (is_wide(P, r[k], work)) wide += (float)r[k].tiles;
+  wide = sum_wave(wide);
+  if ((tid & 63) == 0) s_wide[w] = wide;
+  __syncthreads();
+  wide = 0.f;
+#pragma unroll
+  for (int v = 0; v < NW; ++v) wide += s_wide[v];
+  const int per = pages_per_part<ROWS>(P, work, tiles, wide);
   int n[4] = {0, 0, 0, 0};                  // parts, slots, split tiles, long tiles
   int splits[PER];
 #pragma unroll
