@@ -32,8 +32,8 @@ namespace {
 // product with these is issued, the next values likewise, so one of the two is
 // always on its way, and the registers leave room for more waves, which hide the
 // rest.  Bound by HBM: 32 ragged requests of up to 8K (32/8 heads, d 128, 276 MB)
-// 54.7 us with the join, 5.0 TB/s (a large copy reaches 4.97); one of 128K (28/4 heads,
-// 134 MB) 31.4 us, of which the join 4.
+// 53.7 us with the join, 5.15 TB/s (a large copy reaches 4.97); one of 128K (28/4 heads,
+// 134 MB) 30.2 us, of which the join 4.6.
 template <int D, int DT, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendParams P) {
   constexpr int L = D / 32;                 // 16-byte loads of a lane: keys, and again values
