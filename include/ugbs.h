@@ -493,12 +493,13 @@ UGBS_API int ugbs_cache_plan(const ugbs_cache* c, const int32_t* ctx_lens, const
 
 /* New tokens into the cache.
  *   K, V  : [B, H_kv, rows, d] bf16, 16-byte aligned.
- *   slots : [B, rows] int32 from ugbs_cache_plan: the rows of a request with a
- *           slot come first and follow each other (slot i + 1 is the next token
- *           of the page, or token 0 of another page).  A row whose slot breaks
- *           this, or lies in no page, is not stored; where it would be the first
- *           one in its page, the page's others aren't either.  Rows without a slot
- *           are not stored.  No page may take rows twice in a call, from one request or two.
+ *   slots : [B, rows] int32 from ugbs_cache_plan: rows with a slot follow each
+ *           other (slot i + 1 is the next token of the page, or token 0 of another
+ *           page), but for pages that are none, whose rows have no slot: these rows
+ *           are not stored, and all other pages as ever, whichever are missing.  A row
+ *           whose slot breaks this, or lies in no page, is not stored; where it would be
+ *           the first one in its page, the page's others aren't either.  No page may take
+ *           rows twice in a call, from one request or two.
  *   The scale of a page (per kv head, for keys and for values) is the smallest
  *   power of two s >= 2^-100 with max |x| <= M s over the tokens it was given, M =
  *   448 (e4m3) or 127.  Bytes are x / s, rounded once to nearest, ties to even.

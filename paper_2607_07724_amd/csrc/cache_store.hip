@@ -96,11 +96,20 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
   const int32_t* const slot = slots + (size_t)b * s.rows;
   // the first row's place in its page decides which rows belong to the j-th page touched
   const int s0 = slot[0];
-  if (s0 < 0) return;
-  const int off = s0 % kBlock;
-  const int i0 = max(0, j * kBlock - off);
+  int i0 = 0, t0 = 0;
+  if (s0 >= 0) {
+    t0 = j == 0 ? s0 % kBlock : 0;
+    i0 = max(0, j * kBlock - s0 % kBlock);
+  } else {
+    // no page for the first row: the j-th one begins at the row among 64 j - 63 .. 64 j that is its token 0
+    if (j == 0) return;
+    const int i = j * kBlock - (kBlock - 1) + (tid & 63), x = i < s.rows ? slot[i] : -1;
+    const unsigned long long begins = __ballot(x >= 0 && x % kBlock == 0);
+    if (!begins) return;
+    i0 = j * kBlock - __builtin_clzll(begins);
+  }
   if (i0 >= s.rows) return;
-  const int i1 = min(s.rows, (j + 1) * kBlock - off), t0 = j == 0 ? off : 0;
+  const int i1 = min(s.rows, i0 + kBlock - t0);
   // this thread's 4 tokens and 8 channels; the slots of its rows come with the first one's
   const int cg = tid % CG, tg = tid / CG, c0 = 8 * cg;
   int mine[4];
