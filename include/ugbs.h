@@ -476,8 +476,9 @@ typedef struct ugbs_cache {
  *                is no page).
  *   free_left  : [1] int32 out: the stack's height after the step.
  * In this order: the ceil(ctx / 64) pages of every released request are pushed,
- * request by request and page by page (what passes n_pages is dropped); its
- * kv_len and q_len are 0 and its table row stays as it is.  Then the requests take
+ * request by request and page by page (entries that are no page are passed over,
+ * what passes n_pages is dropped); its kv_len and q_len are 0 and its table row
+ * stays as it is.  Then the requests take
  * the ceil((ctx + new) / 64) - ceil(ctx / 64) pages they need from the top of the
  * stack, in order; a request that needs pages is granted them when its need and
  * those of all requests before it fit, else it adds nothing (q_len 0, kv_len ctx).

@@ -7,7 +7,9 @@
 // every new page has a place of its own in the stack, so no workgroup waits for
 // another: each one forms the sums for itself, and then takes its share of the
 // slots.  Slot i of request b belongs to position ctx_b + i; the slot that
-// begins a page also writes the table's entry.
+// begins a page also writes the table's entry.  Entries of a released request
+// that are no page are not given back: where a request is released the others
+// are counted first, 16 lanes to each (500 requests, 10 of them released: 8.5 -> 10.6 us).
 #include "cache_internal.h"
 
 namespace ugbs {
@@ -48,9 +50,12 @@ __device__ __forceinline__ Request request_of(const PlanParams& P, int b) {
   return r;
 }
 
+__device__ __forceinline__ bool is_page(const PlanParams& P, int32_t x) { return x >= 0 && x < P.s.n_pages; }
+
 __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
   extern __shared__ int s_sum[];            // [B] pages given back before request b, [B] needed before it
   __shared__ int s_wave[2][kThreads / 64];
+  __shared__ int s_gone, s_holes;           // released requests; entries of theirs that are no page
   const int B = P.s.B, tid = threadIdx.x;
   int* const s_back = s_sum;
   int* const s_need = s_sum + B;
@@ -61,8 +66,36 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
 #pragma unroll 4
   for (int b = b0; b < b1; ++b) {
     const Request r = request_of(P, b);
+    s_back[b] = r.back;
     back += r.back;
     need += r.need;
+  }
+  if (tid == 0) s_gone = s_holes = 0;
+  if (__syncthreads_or(back > 0)) {
+    for (int b = b0; b < b1; ++b)
+      if (s_back[b] > 0) s_need[atomicAdd(&s_gone, 1)] = b;       // (in any order)
+    __syncthreads();
+    for (int k = tid / 16; k < s_gone; k += kThreads / 16) {
+      const int b = s_need[k], n = s_back[b];
+      const int32_t* const row = P.table + (size_t)b * P.s.max_pages;
+      int c = 0;
+      for (int p = tid % 16; p < n; p += 8 * 16) {
+        int32_t x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = row[min(p + 16 * i, n - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c += p + 16 * i < n && is_page(P, x[i]);
+      }
+#pragma unroll
+      for (int o = 1; o < 16; o *= 2) c += __shfl_xor(c, o);
+      if (tid % 16 == 0 && c < n) {
+        s_back[b] = c;
+        s_holes = 1;
+      }
+    }
+    __syncthreads();
+    back = 0;
+    for (int b = b0; b < b1; ++b) back += s_back[b];
   }
   const int back_in = scan_add(back), need_in = scan_add(need);
   const int w = tid >> 6;
@@ -85,6 +118,7 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
   int taken = 0;                                             // pages granted up to this thread's last request
   for (int b = b0; b < b1; ++b) {
     const Request r = request_of(P, b);
+    const int r_back = s_back[b];
     s_back[b] = back_at;
     s_need[b] = need_at;
     const bool ok = r.need == 0 || need_at + r.need <= stock;
@@ -93,7 +127,7 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
       P.kv_lens[b] = r.gone ? 0 : r.ctx + (ok ? r.q : 0);
       P.q_lens[b] = ok ? r.q : 0;
     }
-    back_at += r.back;
+    back_at += r_back;
     need_at += r.need;
   }
   __syncthreads();
@@ -109,14 +143,26 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
     }
   }
   // the page at place j of the pages given back
-  auto returned = [&](int j) {
+  auto returned = [&](int j) -> int32_t {
     int lo = 0, hi = B - 1;                 // the last request with s_back[b] <= j
     while (lo < hi) {
       const int mid = (lo + hi + 1) / 2;
       if (s_back[mid] <= j) lo = mid;
       else hi = mid - 1;
     }
-    return P.table[(size_t)lo * P.s.max_pages + (j - s_back[lo])];
+    const int32_t* const row = P.table + (size_t)lo * P.s.max_pages;
+    int k = j - s_back[lo];
+    if (!s_holes) return row[k];
+#pragma unroll 1
+    for (int p = 0; p < P.s.max_pages; p += 16) {
+      int32_t x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[i] = row[min(p + i, P.s.max_pages - 1)];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (p + i < P.s.max_pages && is_page(P, x[i]) && k-- == 0) return x[i];
+    }
+    return -1;
   };
   const int stride = gridDim.x * kThreads, first = blockIdx.x * kThreads + tid;
   for (int j = first; j < stock - held0; j += stride) P.free_pages[held0 + j] = returned(j);
@@ -146,7 +192,7 @@ __global__ void __launch_bounds__(kThreads) cache_plan_kernel(PlanParams P) {
       if (place[k] >= 0 && new_page[k] && place[k] % kBlock == 0)
         P.table[(size_t)(at / rows) * P.s.max_pages + place[k] / kBlock] = page[k];
       // an entry that is no page gives no slot
-      P.slots[at] = place[k] >= 0 && page[k] >= 0 && page[k] < P.s.n_pages ? page[k] * kBlock + place[k] % kBlock : -1;
+      P.slots[at] = place[k] >= 0 && is_page(P, page[k]) ? page[k] * kBlock + place[k] % kBlock : -1;
     }
   }
 }

@@ -10,7 +10,7 @@ import cache_oracle as co
 import paper_2607_07724_amd as ugbs
 
 from gpu_helpers import bf16_to_f64, dev, dev_bf16, host, host_bits
-from test_gpu_cache import I32, PAGE, Contents, bf16, pages, reference, run_attend
+from test_gpu_cache import I32, PAGE, Contents, _plan_case, _run_plan, bf16, pages, reference, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -85,3 +85,70 @@ def test_pages_that_are_missing_take_nothing_from_the_others(rows, d, dtype):
         n = int(want[3][b])
         ref, tol = reference(x, b, Qv[b], int(want[2][b]), n, 1 / math.sqrt(d), True)
         assert (np.abs(O[b, :, :n] - ref[:, :n]) <= tol[:, :n]).all(), b
+
+
+# ---------------------------------------------------------------- what a released request gives back
+
+def plan_past_holes(ctx, new, stack, count, table, rows):
+    """The oracle's plan after the rows of released requests were closed up over what is no page."""
+    closed, ctx = table.copy(), ctx.copy()
+    gone = [b for b in range(len(ctx)) if new[b] == -1 and 0 <= ctx[b] <= PAGE * table.shape[1]]
+    for b in gone:
+        row = [p for p in table[b, :pages(int(ctx[b]))] if 0 <= p < len(stack)]
+        closed[b, :len(row)], ctx[b] = row, PAGE * len(row)
+    out = co.plan(ctx, new, stack, count, closed, rows)
+    out[1][gone] = table[gone]
+    return out
+
+
+@pytest.mark.parametrize("B,max_pages,rows,stock,wild,room", [
+    (1, 1, 1, 1, False, 50), (2, 300, 64, 1, False, 50), (5, 4, 100, 0.5, False, 1), (64, 6, 3, 1, False, 0), (65, 9, 65, 0, False, 50),
+    (257, 5, 7, 0.3, True, 50), (1000, 3, 130, 0, True, 50), (4096, 2, 1, 0.5, True, 50), (30, 150, 2000, 0, False, 50)])
+def test_entries_that_are_no_page_are_not_given_back(B, max_pages, rows, stock, wild, room):
+    g = np.random.default_rng(B + max_pages)
+    for share in (0.02, 0.3, 1.0):
+        ctx, new, stack, count, table = _plan_case(g, B, max_pages, rows, stock, wild)
+        new[g.random(B) < 0.3] = -1
+        new[-1] = -1
+        hole = (new == -1)[:, None] & (g.random(table.shape) < share) & (table >= 0)
+        table[hole] = g.choice([-1, len(stack), 2 ** 31 - 1, -2 ** 31], hole.sum())
+        stack = stack[:len(stack) - 50 + room]
+        count = min(count, len(stack))
+        if room == 0 and len(stack):                     # nearly full: what passes it is dropped
+            stack, count = g.permutation(len(stack)).astype(I32), len(stack) - 1
+        got = _run_plan(ctx, new, stack, count, table, rows)
+        want = plan_past_holes(ctx, new, stack, count, table, rows)
+        for name, a, b in zip(("free_pages", "table", "kv_lens", "q_lens", "slots", "free_left"), got, want):
+            assert np.array_equal(a, b), (share, name)
+
+
+def test_a_request_after_one_with_a_hole_gets_pages():
+    """A request of two pages, of which one is none, is released; the next one takes the other and a free
+    one, is stored, and attends to what is its own."""
+    g = np.random.default_rng(70)
+    d, rows = 128, 128
+    x = Contents(g, [64, 0], 1, d, 0, max_pages=2, n_pages=8)
+    page = int(x.table[0, 0])
+    free = (page + 3) % 8
+    ctx, new = np.array([128, 0], I32), np.array([-1, 128], I32)
+    stack = np.full(8, -1, I32)
+    stack[0] = free
+    c = ugbs.Cache.make(2, 4, 1, d, 8, 2, rows=rows)
+    cache, scales, table = x.device()
+    kv, q, left = (torch.full((n,), -9, dtype=torch.int32, device="cuda") for n in (2, 2, 1))
+    slots = torch.full((2, rows), -9, dtype=torch.int32, device="cuda")
+    ugbs.ugbs_cache_plan(c, dev(ctx), dev(new), dev(stack), dev(np.array([1], I32)), table, kv, q, slots, left)
+    assert host(table).tolist() == [[page, -1], [page, free]] and int(left.item()) == 0
+    assert kv.tolist() == [0, 128] and q.tolist() == [0, 128]
+    Kb, K = bf16(g.normal(0, 1, (2, 1, rows, d)))
+    Vb, V = bf16(g.normal(0, 1, (2, 1, rows, d)))
+    ugbs.ugbs_cache_store(c, dev_bf16(Kb), dev_bf16(Vb), slots, cache, scales)
+    x.raw, x.scales = co.store(K, V, host(slots), x.raw, x.scales, 0)
+    x.table = host(table)
+    Qb, Qv = bf16(g.normal(0, 1, (2, 4, rows, d)))
+    O = torch.zeros((2, 4, rows, d), dtype=torch.bfloat16, device="cuda")
+    ugbs.ugbs_cache_attend(c, dev_bf16(Qb), cache, scales, table, kv, q, O,
+                           torch.empty(max(256, ugbs.ugbs_cache_workspace_bytes(c)), dtype=torch.uint8, device="cuda"))
+    got = bf16_to_f64(host_bits(O))
+    want, tol = reference(x, 1, Qv[1], 128, 128, 1 / math.sqrt(d), True)
+    assert (np.abs(got[1] - want) <= tol).all() and not got[0].any()
