@@ -437,10 +437,14 @@ UGBS_API size_t ugbs_workspace_bytes(const ugbs_problem* p);
  * page holds behind its request's last token is never used.
  * A request's pages are listed in its row of
  *   table  : [B, max_pages] int32: position j of request b lies in page
- *            table[b, j / 64] at token j % 64.  Requests may list the same page
- *            (a common prefix) as long as only reads reach it.  An entry outside
- *            [0, n_pages) is no page: what would lie there is left out (its keys
- *            are not attended, nothing is stored, loads give 0).
+ *            table[b, j / 64] at token j % 64.  An entry outside [0, n_pages) is no
+ *            page: what would lie there is left out (its keys are not attended,
+ *            nothing is stored, loads give 0).  Requests may list the same page (a
+ *            common prefix) as long as only reads reach it and it is given back once:
+ *            the pages of a request that others go on listing have to leave its row
+ *            (entries of -1, say) before it is released, and two that are released
+ *            together must not list one page both.  Nothing counts a page's users: it
+ *            would be granted while in use, or to two requests.
  * One step of a batch, per layer but for the first call:
  *   ugbs_cache_plan   (lengths)             -> table, slots, kv_lens, q_lens
  *   ugbs_cache_store  (K, V, slots)         -> cache, scales

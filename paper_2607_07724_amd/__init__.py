@@ -511,7 +511,7 @@ def _cache_arrays(c, cache, scales, pages, Hkv, d, index, dev):
 def ugbs_cache_plan(c: Cache, ctx_lens, new_lens, free_pages, free_count, table, kv_lens, q_lens, slots, free_left,
                     stream=None):
     """A step's pages, slots and lengths from the requests' lengths [B] int32 (new_lens CACHE_RELEASE: the
-    request's pages go back) and the stack free_pages [n_pages] of height free_count [1]: table
+    request's pages go back; those that other requests list too have to leave its table row first) and the stack free_pages [n_pages] of height free_count [1]: table
     [B,max_pages] is extended, kv_lens, q_lens [B], slots [B,rows] and free_left [1] are written."""
     _get_torch()
     x, dev = _device_of("ctx_lens", ctx_lens)

@@ -10,7 +10,7 @@ import cache_oracle as co
 import paper_2607_07724_amd as ugbs
 
 from gpu_helpers import bf16_to_f64, dev, dev_bf16, host, host_bits
-from test_gpu_cache import I32, PAGE, Contents, _plan_case, _run_plan, bf16, pages, reference, run_attend
+from test_gpu_cache import I32, PAGE, Contents, Mirror, _check_step, _plan_case, _run_plan, bf16, pages, reference, run_attend
 
 pytestmark = pytest.mark.gpu
 
@@ -152,3 +152,40 @@ def test_a_request_after_one_with_a_hole_gets_pages():
     got = bf16_to_f64(host_bits(O))
     want, tol = reference(x, 1, Qv[1], 128, 128, 1 / math.sqrt(d), True)
     assert (np.abs(got[1] - want) <= tol).all() and not got[0].any()
+
+
+def test_a_common_prefix_is_given_back_once():
+    """Request 1 lists the prompt's first page of request 0, and is released without it: request 0 goes on,
+    request 2 takes what came back, and at the end every page is free once."""
+    g = np.random.default_rng(80)
+    B, H, Hkv, d, n_pages, max_pages = 3, 4, 2, 64, 9, 4
+    c0 = ugbs.Cache.make(B, H, Hkv, d, n_pages, max_pages, rows=150)
+    cbufs, step, mir = ugbs.CacheBuffers(c0), ugbs.CacheStep(c0), Mirror(c0)
+    cbufs.cache.zero_()
+    cbufs.scales.zero_()
+
+    def one(rows, new):
+        c = ugbs.Cache.make(B, H, Hkv, d, n_pages, max_pages, rows=rows)
+        new = np.array(new, I32)
+        (Qb, Qv), (Kb, K), (Vb, V) = (bf16(g.normal(0, 1, (B, h, rows, d))) for h in (H, Hkv, Hkv))
+        O = torch.zeros((B, H, rows, d), dtype=torch.bfloat16, device="cuda")
+        step.plan(c, dev(new))
+        ugbs.cache_layer(c, dev_bf16(Qb), dev_bf16(Kb), dev_bf16(Vb), O, cbufs, step)
+        mir.stack, mir.table, mir.kv, mir.q, slots, mir.count = plan_past_holes(mir.kv, new, mir.stack, mir.count, mir.table, rows)
+        mir.raw, mir.scales = store_past_holes(K, V, slots, mir.raw, mir.scales, mir.dtype)
+        assert np.array_equal(host(step.table), mir.table) and np.array_equal(host(step.kv_lens), mir.kv)
+        assert int(step.free_left.item()) == mir.count and np.array_equal(host(step.free_pages), mir.stack)
+        _check_step(mir, O, Qv, 1 / math.sqrt(d))
+
+    one(128, [128, 0, 0])
+    step.table[1, 0] = step.table[0, 0]
+    step.kv_lens[1] = 64
+    mir.table[1, 0], mir.kv[1] = mir.table[0, 0], 64
+    one(90, [70, 90, 0])
+    one(1, [1, 1, 0])
+    step.table[1, 0] = -1
+    mir.table[1, 0] = -1
+    one(150, [5, -1, 150])
+    one(1, [1, 0, 1])
+    one(1, [-1, 0, -1])
+    assert int(step.free_left.item()) == n_pages and sorted(step.free_pages.tolist()) == list(range(n_pages))
