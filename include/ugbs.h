@@ -508,6 +508,9 @@ UGBS_API int ugbs_cache_plan(const ugbs_cache* c, const int32_t* ctx_lens, const
  *   The scale of a page (per kv head, for keys and for values) is the smallest
  *   power of two s >= 2^-100 with max |x| <= M s over the tokens it was given, M =
  *   448 (e4m3) or 127.  Bytes are x / s, rounded once to nearest, ties to even.
+ *   Inputs have to be finite here too.  Those that are not leave the other tokens as
+ *   they are: they do not count for the scale, infinities are kept as +-M s and NaN as
+ *   0, so a cache holds finite numbers only and attention over it does not show them.
  *   A call whose first token of a page is token 0 starts the page anew; one that
  *   goes on behind tokens 0..t-1 keeps their scale or raises it, and then rounds
  *   their bytes times s_old / s_new again (exact for e4m3 but for its subnormals). */

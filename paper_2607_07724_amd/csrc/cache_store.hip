@@ -14,6 +14,8 @@
 // out of one thread as a dword.  A whole page is put together in LDS and
 // written 16 bytes a lane; in a page that held tokens before, or is not filled,
 // bytes are written one token at a time and the others stay.
+#include <type_traits>
+
 #include "cache_internal.h"
 
 namespace ugbs {
@@ -29,6 +31,19 @@ __device__ __forceinline__ float bf16_at(const uint4& v, int e) {
 __device__ __forceinline__ uint32_t abs_max2(uint32_t m, uint32_t w) {
   const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
   return max(m, max(lo, hi));
+}
+
+// x, opaque to the compiler: what a rare branch forms of it is not kept in registers for it from before.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// The same of numbers that are finite.
+__device__ __forceinline__ uint32_t finite_max2(uint32_t m, uint32_t w) {
+  w = here(w);
+  const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;
+  return max(m, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
 }
 
 // The scale of a page whose largest |x| has the bf16 pattern a.
@@ -140,20 +155,36 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
     ka = abs_max2(abs_max2(abs_max2(abs_max2(ka, k[e].x), k[e].y), k[e].z), k[e].w);
     va = abs_max2(abs_max2(abs_max2(abs_max2(va, v[e].x), v[e].y), v[e].z), v[e].w);
   }
+  int whole = 0;
+  auto page_max = [&]() {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    ka = max(ka, (uint32_t)__shfl_xor((int)ka, o));
-    va = max(va, (uint32_t)__shfl_xor((int)va, o));
-  }
-  if ((tid & 63) == 0) {
-    s_amax[w][0] = ka;
-    s_amax[w][1] = va;
-  }
-  const int whole = __syncthreads_and(live == 15u);
+    for (int o = 1; o < 64; o *= 2) {
+      ka = max(ka, (uint32_t)__shfl_xor((int)ka, o));
+      va = max(va, (uint32_t)__shfl_xor((int)va, o));
+    }
+    if ((tid & 63) == 0) {
+      s_amax[w][0] = ka;
+      s_amax[w][1] = va;
+    }
+    whole = __syncthreads_and(live == 15u);
 #pragma unroll
-  for (int x = 0; x < NW; ++x) {
-    ka = max(ka, s_amax[x][0]);
-    va = max(va, s_amax[x][1]);
+    for (int x = 0; x < NW; ++x) {
+      ka = max(ka, s_amax[x][0]);
+      va = max(va, s_amax[x][1]);
+    }
+  };
+  page_max();
+  // a number that is not finite must not take the scale, and with it the page's other tokens, along
+  const bool finite = __builtin_amdgcn_readfirstlane(max(ka, va)) < 0x7f80;
+  if (!finite) {
+    ka = va = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      ka = finite_max2(finite_max2(finite_max2(finite_max2(ka, k[e].x), k[e].y), k[e].z), k[e].w);
+      va = finite_max2(finite_max2(finite_max2(finite_max2(va, v[e].x), v[e].y), v[e].z), v[e].w);
+    }
+    __syncthreads();
+    page_max();
   }
   float ks = scale_for<DT>(ka), vs = scale_for<DT>(va);
   uint8_t* const kp = cache + ((size_t)page * s.Hkv + kvh) * 2 * (kBlock * D);
@@ -189,16 +220,21 @@ __global__ void __launch_bounds__(2 * D) cache_store_kernel(CacheShape s, const 
   const float ki = 1.0f / ks, vi = 1.0f / vs;
   uint2 kb[4];
   uint32_t vb[8];
+  auto convert = [&](auto all_finite) {     // (else NaN become 0, infinities the largest number)
+    auto at = [&](const uint4& from, int c, float inv) {
+      if constexpr (all_finite.value) return bf16_at(from, c) * inv;
+      const float x = bf16_at(make_uint4(here(from.x), here(from.y), here(from.z), here(from.w)), c) * inv;
+      return x == x ? x : 0.f;
+    };
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float x[8];
+    for (int e = 0; e < 4; ++e)
+      kb[e] = make_uint2(to_bytes<DT>(at(k[e], 0, ki), at(k[e], 1, ki), at(k[e], 2, ki), at(k[e], 3, ki)),
+                         to_bytes<DT>(at(k[e], 4, ki), at(k[e], 5, ki), at(k[e], 6, ki), at(k[e], 7, ki)));
 #pragma unroll
-    for (int c = 0; c < 8; ++c) x[c] = bf16_at(k[e], c) * ki;
-    kb[e] = make_uint2(to_bytes<DT>(x[0], x[1], x[2], x[3]), to_bytes<DT>(x[4], x[5], x[6], x[7]));
-  }
-#pragma unroll
-  for (int c = 0; c < 8; ++c)
-    vb[c] = to_bytes<DT>(bf16_at(v[0], c) * vi, bf16_at(v[1], c) * vi, bf16_at(v[2], c) * vi, bf16_at(v[3], c) * vi);
+    for (int c = 0; c < 8; ++c) vb[c] = to_bytes<DT>(at(v[0], c, vi), at(v[1], c, vi), at(v[2], c, vi), at(v[3], c, vi));
+  };
+  if (finite) convert(std::true_type{});
+  else convert(std::false_type{});
 
   if (whole) {
 #pragma unroll
