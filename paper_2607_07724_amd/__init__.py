@@ -502,6 +502,8 @@ def _device_of(name, t):
 
 
 def _cache_arrays(c, cache, scales, pages, Hkv, d, index, dev):
+    if cache is None:
+        raise ValueError("cache is required")
     if cache.dtype.itemsize != 1:
         raise ValueError(f"cache: dtype {cache.dtype} is not of 8 bits")
     return (_addr("cache", cache, (pages, Hkv, 2, BLOCK * d), (cache.dtype,), index, dev),
