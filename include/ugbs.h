@@ -450,7 +450,8 @@ UGBS_API size_t ugbs_workspace_bytes(const ugbs_problem* p);
  *   ugbs_cache_store  (K, V, slots)         -> cache, scales
  *   ugbs_cache_attend (Q, cache, ...)       -> O
  * and ugbs_cache_load gives cached tokens back as bf16 K and V (exactly), for
- * the prefill entry points above.  Lengths stay on the device, so a step can be
+ * the prefill entry points above (over a whole cached prompt: these take as many
+ * query rows as keys).  Lengths stay on the device, so a step can be
  * captured in a HIP graph and replayed as lengths grow. */
 typedef enum { UGBS_E4M3 = 0, UGBS_INT8 = 1 } ugbs_cache_type;
 
@@ -538,7 +539,7 @@ UGBS_API int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float
  *   for the second product.  With e4m3, d 128 or 256 and more than 32 (16 at d 256)
  *   query rows to a kv head (rows H / H_kv), a query channel enters the first product as
  *   two e4m3 numbers: exact but for what lies below 2^-22 of the largest of its 32
- *   channels (32 j .. 32 j + 31).  A row that sees no key (p_i < 0, or no page)
+ *   channels (32 j .. 32 j + 31), or below 2^-115.  A row that sees no key (p_i < 0, or no page)
  *   gives 0.  Results do not depend on timing: equal calls on equal GPUs agree bit
  *   for bit.
  *   Q, O      : [B, H, rows, d] bf16, 16-byte aligned.  Rows q_lens[b] and up are

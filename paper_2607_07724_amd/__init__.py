@@ -662,7 +662,8 @@ class CacheStep:
 
 def prefill_cached(p: Problem, c: Cache, Q, K, V, O, bufs: Buffers, cbufs: CacheBuffers, step: CacheStep, stream=None):
     """prefill of prompts that begin with this step, their K and V kept in the cache (c.rows == p.seq_len;
-    step.plan comes first)."""
+    step.plan comes first).  Of a prompt of fewer tokens than p.seq_len (step.q_lens) those are kept; the
+    prefill takes the rows behind them as any others, the route among it."""
     if c.rows != p.seq_len:
         raise ValueError(f"the cache's rows ({c.rows}) are not the prompt's {p.seq_len}")
     prefill(p, Q, K, V, O, bufs, stream)

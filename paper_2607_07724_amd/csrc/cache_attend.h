@@ -5,8 +5,8 @@
 
 namespace ugbs {
 
-// Parts a call aims at, at most, and the pages of a part, at least: 64 KiB, four pages
-// (one request of 4000 tokens at d 128: 11.3 us with 8 pages, 10.1 with 4; of 8000 at
+// Parts a call aims at, at most, and the pages of a part, at least: 64 KiB at d 64 and 128,
+// 128 KiB at d 256 (one request of 4000 tokens at d 128: 11.3 us with 8 pages, 10.1 with 4; of 8000 at
 // d 256: 11.7 with 4, 12.4 with 2).
 constexpr int kTarget = 512;
 constexpr int min_pages(int d) { return d == 64 ? 8 : 4; }

@@ -13,9 +13,10 @@
 // before their rounding to bf16 (2^-8 relative at most).
 //
 // Work is split along the pages where there are few rows: with W the pages of
-// all tiles, a tile of n pages goes to ceil(n / X) workgroups, X just above W / 512
-// (at least 64 KiB), so that a long request among short ones does not hold
-// up the call.  The lengths are on the device; each wave forms the sums over
+// all tiles, a tile of n pages goes to ceil(n / X) workgroups, X just above W / A,
+// A 512 less a share of the long tiles, 256 at least, and X not below the least
+// pages of a part (64 or 128 KiB, twice that from 256 tiles on), so that a long
+// request among short ones does not hold up the call.  The lengths are on the device; each wave forms the sums over
 // the requests for itself.  Parts leave their sums and maxima in the workspace,
 // and a second launch joins them, in the order of the pages.
 #include <type_traits>
@@ -32,8 +33,8 @@ namespace {
 // product with these is issued, the next values likewise, so one of the two is
 // always on its way, and the registers leave room for more waves, which hide the
 // rest.  Bound by HBM: 32 ragged requests of up to 8K (32/8 heads, d 128, 276 MB)
-// 53.7 us with the join, 5.15 TB/s (a large copy reaches 4.97); one of 128K (28/4 heads,
-// 134 MB) 30.2 us, of which the join 4.6.
+// 53 us with the join, 5.2 TB/s (large copies reach 4.7 to 6.1); one of 128K (28/4 heads,
+// 134 MB) 30.3 us, of which the join 4.6.
 template <int D, int DT, int RT, int NW>
 __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendParams P) {
   constexpr int L = D / 32;                 // 16-byte loads of a lane: keys, and again values

@@ -7,7 +7,7 @@
 // keys of 128 or 256 channels are operands as they are (see split_row); the values, and
 // all other bytes, are widened to bf16 once for the 64 rows.  Bound by the vector unit
 // (exponentials, widening) beside the matrix cores: two pieces of 1024 tokens on up to 33K
-// (32/8 heads, d 128) 617-642 us, 1.10-1.14 PFLOP/s.
+// (32/8 heads, d 128) 608-657 us, 1.07-1.16 PFLOP/s.
 // O alone takes D registers a row tile of 16, so the bytes wait in LDS: direct loads,
 // 1 KiB each, land in the order in which lanes read them, without bank conflicts.  The
 // values' loads go out one by one between the matrix instructions of S, the next keys'
@@ -156,9 +156,9 @@ cache_tiles_kernel(CacheAttendParams P) {
   // with a power of two for each 32 channels of a row, the instruction's own scales, give
   // the bf16 number back: the largest of the 32 is brought to 128..255, hi is a number's
   // nearest with 4 significant bits, and what is left has at most 4.  (Numbers below 2^-13
-  // of the largest of their 32 lose what lies below 2^-22 of it.)  So the keys' bytes are
-  // operands as they are; on this instruction two such products cost what one in bf16 does
-  // (pieces of 1024 tokens, d 128: 645 -> 611 us, d 256: 724 -> 668).
+  // of the largest of their 32, taken as 2^-93 at least, lose what lies below 2^-22 of it.)
+  // So the keys' bytes are operands as they are; on this instruction two such products cost
+  // what one in bf16 does (pieces of 1024 tokens, d 128: 645 -> 611 us, d 256: 724 -> 668).
   uint4 bq[QR][2 * E];                      // F8: [E / 2][hi, lo][2], 16 channels each
   constexpr int C = F8 ? E / 2 : 1;         // 128-channel steps
   uint32_t q_hi[C] = {}, q_lo[C];           // F8: exponents (E8M0) of row tile rt's hi and lo in byte rt
