@@ -63,6 +63,13 @@ __device__ __forceinline__ int scan_add(int x) {
   return x;
 }
 
+// x, opaque to the compiler: what follows from it is formed where it is used, not kept
+// in registers over a loop or from before a rare branch.
+__device__ __forceinline__ uint32_t here(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // 16 bytes that are read once: not kept in the caches (a decode step over 300 MB:
 // 64 -> 57 us).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

@@ -33,13 +33,7 @@ __device__ __forceinline__ uint32_t abs_max2(uint32_t m, uint32_t w) {
   return max(m, max(lo, hi));
 }
 
-// x, opaque to the compiler: what a rare branch forms of it is not kept in registers for it from before.
-__device__ __forceinline__ uint32_t here(uint32_t x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
-// The same of numbers that are finite.
+// The same of numbers that are finite (a rare branch: see here()).
 __device__ __forceinline__ uint32_t finite_max2(uint32_t m, uint32_t w) {
   w = here(w);
   const uint32_t lo = w & 0x7fffu, hi = (w >> 16) & 0x7fffu;

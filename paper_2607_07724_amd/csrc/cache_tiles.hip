@@ -36,13 +36,6 @@ __device__ __forceinline__ void dma16_cache(const uint8_t* base, uint32_t voff, 
                  : "memory");
 }
 
-// x, opaque to the compiler: what follows from it is formed where it is used, not kept
-// in registers over the loop.
-__device__ __forceinline__ uint32_t here(uint32_t x) {
-  asm volatile("" : "+v"(x));
-  return x;
-}
-
 // f(0) .. f(N - 1) with indexes that are constants
 template <int N, int I = 0, class F>
 __device__ __forceinline__ void each(F f) {
