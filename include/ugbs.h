@@ -26,6 +26,9 @@
  *   ugbs_attend_bitmap(Q, K, V, bitmap)      -> O
  * and, for the tokens after the prompt, a paged cache in 8 bits:
  *   ugbs_cache_plan, ugbs_cache_store, ugbs_cache_attend, ugbs_cache_load
+ * Before them, from a projection's rows (norms of heads, rotation by position):
+ *   ugbs_heads_split  (rows)                 -> Q, K, V
+ *   ugbs_heads_store  (rows, slots)          -> Q, cache
  * No call synchronises the device; none allocates device memory.
  *
  * Diagnostics (Appendix D: sigma as a best-arm identification index), off
@@ -71,7 +74,7 @@ extern "C" {
 #define UGBS_API
 #endif
 
-#define UGBS_ABI_VERSION 11
+#define UGBS_ABI_VERSION 12
 #define UGBS_BLOCK 64          /* BLOCK_M = BLOCK_N = 64 tokens (Section 3.1, 3.2) */
 #define UGBS_MAX_BLOCKS 4096   /* N_B <= 4096, i.e. N <= 262144 */
 #define UGBS_MAX_BLOCKS_ROWS 2048 /* ugbs_select_rows, ugbs_bai_tiles, ugbs_bai_heads: N_B <= 2048 */
@@ -80,13 +83,16 @@ extern "C" {
 #define UGBS_MAX_REQUESTS 4096 /* requests of a batch over the cache */
 #define UGBS_MAX_PAGES (1 << 24) /* pages of a cache (2^30 tokens) */
 #define UGBS_MAX_WIDTH (1 << 20) /* rows of a tensor that ugbs_cache_load fills */
+#define UGBS_MAX_TOKENS (1 << 23) /* batch * rows of ugbs_heads */
+#define UGBS_MAX_AXES 4        /* position axes of ugbs_heads */
 #define UGBS_CACHE_RELEASE (-1) /* ugbs_cache_plan: the request gives its pages back */
 #define UGBS_ROUTE_SCRATCH_BYTES (1u << 20) /* device scratch of ugbs_route_noalloc, per GPU */
 
 typedef enum {
   UGBS_OK = 0,
   UGBS_ERR_NULL = 1,      /* a required pointer is NULL */
-  UGBS_ERR_SHAPE = 2,     /* batch/heads/seq_len/head_dim/block/kv_width/n_pages/max_pages/rows/width invalid */
+  UGBS_ERR_SHAPE = 2,     /* batch/heads/seq_len/head_dim/block/kv_width/n_pages/max_pages/rows/width invalid;
+                             ugbs_heads_store: the two descriptions disagree */
   UGBS_ERR_BUDGET = 3,    /* k_budget < 3, rho outside [1, 8], or rho k_budget > 4096 */
   UGBS_ERR_Q = 4,         /* q outside [0, 1] or NaN */
   UGBS_ERR_BACKBONE = 5,  /* backbone not one of ugbs_backbone */
@@ -96,7 +102,9 @@ typedef enum {
   UGBS_ERR_SCALE = 9,     /* softmax_scale negative, NaN or infinite */
   UGBS_ERR_SCRATCH = 10,  /* the problem needs more than the static scratch of ugbs_route_noalloc */
   UGBS_ERR_DTYPE = 11,    /* dtype not one of ugbs_cache_type */
-  UGBS_ERR_ALIAS = 12     /* an output of ugbs_cache_plan is one of its other arrays */
+  UGBS_ERR_ALIAS = 12,    /* an output of ugbs_cache_plan is one of its other arrays */
+  UGBS_ERR_ROTARY = 13,   /* rot_dim, pairs, axes, norm_eps or rot_gain invalid */
+  UGBS_ERR_STRIDE = 14    /* a stride of ugbs_rows is not a multiple of 8 */
 } ugbs_status;
 
 /* Block-scoring backbone (Section 3.1).
@@ -555,6 +563,70 @@ UGBS_API int ugbs_cache_attend(const ugbs_cache* c, const void* Q, const void* c
 
 /* Bytes of device workspace of ugbs_cache_attend (0 if c is invalid). */
 UGBS_API size_t ugbs_cache_workspace_bytes(const ugbs_cache* c);
+
+/* ---- From a projection's rows to heads -----------------------------------------
+ * A projection gives a token's queries, keys and values next to each other; the
+ * entry points above take them by heads, queries and keys normed and rotated by
+ * position.  Both steps and the change of order are one pass here.
+ *
+ * Head h of token i of request b, d numbers x in a row, becomes
+ *   y_c = x_c / sqrt(mean_c x_c^2 + norm_eps) w_c       (queries and keys with a weight w, else y = x)
+ * and, of queries and keys, channels 0 .. rot_dim - 1 are rotated in pairs j = 0 .. rot_dim / 2 - 1,
+ *   (y_a, y_b) -> rot_gain (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position freqs[j],
+ * a, b = j, j + rot_dim / 2 (UGBS_HALVES) or 2 j, 2 j + 1 (UGBS_NEIGHBOURS).  Values stay
+ * as they are.  In fp32, angles in 64 bits (t is off by at most 2^-51 |t| + 2^-23), rounded to bf16
+ * once. */
+typedef enum { UGBS_HALVES = 0, UGBS_NEIGHBOURS = 1 } ugbs_pairs;
+
+typedef struct ugbs_heads {
+  int32_t batch;        /* B requests, 1..UGBS_MAX_REQUESTS */
+  int32_t n_heads;      /* H >= 1, a multiple of n_kv_heads */
+  int32_t n_kv_heads;   /* H_kv >= 1, H + 2 H_kv <= 4096 */
+  int32_t head_dim;     /* d: 64, 128 or 256 */
+  int32_t rows;         /* tokens of a request, >= 1, batch * rows <= UGBS_MAX_TOKENS */
+  int32_t rot_dim;      /* channels that are rotated: 0..d, a multiple of 16 */
+  int32_t pairs;        /* ugbs_pairs */
+  int32_t axes;         /* axes of a position, 1..UGBS_MAX_AXES */
+  float norm_eps;       /* >= 0, finite */
+  float rot_gain;       /* of cos and sin (some long-context scalings need one); 0 means 1 */
+} ugbs_heads;
+
+/* Rows of bf16 heads: head h of token i of request b begins at element
+ * b batch + i token + h head behind `at`.  16-byte aligned, strides multiples of 8.  Parts of
+ * one packed projection, gates between the heads and rows read twice (stride 0) are all fine. */
+typedef struct ugbs_rows {
+  const void* at;
+  int64_t batch, token, head;
+} ugbs_rows;
+
+/* Rows to queries, keys and values by heads.
+ *   q, k, v   : H, H_kv and H_kv heads.
+ *   q_norm, k_norm : [d] fp32, 16-byte aligned, the norms' weights; either may be NULL (no norm).
+ *   freqs     : [rot_dim / 2] fp64, 8-byte aligned, angle per position of each pair (may
+ *               be NULL with rot_dim 0).
+ *   positions : [axes, B, rows] int32 or NULL: token i of request b then is at position
+ *               first[b] + i on every axis.
+ *   axis      : [rot_dim / 2] int32, the axis that each pair goes by (taken as 0..axes-1), or
+ *               NULL: all by axis 0.  Not used without positions.
+ *   first     : [B] int32 or NULL (0); ctx_lens of a cache's step, say.  Not used with positions.
+ *   lens      : [B] int32, tokens of each request (taken as 0..rows), or NULL: rows.  The rows
+ *               behind them are neither read nor written.
+ *   Q         : [B, H, rows, d], K, V: [B, H_kv, rows, d] bf16, 16-byte aligned; they overlap
+ *               nothing that the call reads. */
+UGBS_API int ugbs_heads_split(const ugbs_heads* h, const ugbs_rows* q, const ugbs_rows* k, const ugbs_rows* v,
+                              const float* q_norm, const float* k_norm, const double* freqs, const int32_t* positions,
+                              const int32_t* axis, const int32_t* first, const int32_t* lens, void* Q, void* K, void* V,
+                              void* stream);
+
+/* The same, keys and values into the cache: Q is ugbs_heads_split's, and cache and scales become
+ * what ugbs_cache_store makes of its K and V, byte for byte, which are not written otherwise.
+ *   h, c      : of one batch: batch, heads, head_dim and rows are the same.
+ *   lens      : as above, of the queries; which keys and values are kept goes by slots.
+ *   slots, cache, scales : as for ugbs_cache_store. */
+UGBS_API int ugbs_heads_store(const ugbs_heads* h, const ugbs_cache* c, const ugbs_rows* q, const ugbs_rows* k,
+                              const ugbs_rows* v, const float* q_norm, const float* k_norm, const double* freqs,
+                              const int32_t* positions, const int32_t* axis, const int32_t* first, const int32_t* lens,
+                              void* Q, const int32_t* slots, void* cache, float* scales, void* stream);
 
 /* Static, human-readable text for a ugbs_status value. */
 UGBS_API const char* ugbs_status_string(int status);

@@ -26,11 +26,13 @@ __all__ = [
     "ugbs_quest_scores_valu",
     "E4M3", "INT8", "CACHE_RELEASE", "Cache", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
     "ugbs_cache_attend", "ugbs_cache_workspace_bytes", "CacheBuffers", "CacheStep", "prefill_cached", "cache_layer",
+    "HALVES", "NEIGHBOURS", "Heads", "ugbs_heads_split", "ugbs_heads_store",
 ]
 
 KMEAN, QUEST = 0, 1
 E4M3, INT8 = 0, 1
 CACHE_RELEASE = -1
+HALVES, NEIGHBOURS = 0, 1
 BLOCK = 64
 MAX_BLOCKS = 4096
 MAX_BLOCKS_ROWS = 2048
@@ -106,6 +108,25 @@ class Cache(ctypes.Structure):
                 f"dtype={'int8' if self.dtype == INT8 else 'e4m3'})")
 
 
+class Heads(ctypes.Structure):
+    """Mirror of ``ugbs_heads`` (include/ugbs.h)."""
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "n_heads", "n_kv_heads", "head_dim", "rows", "rot_dim", "pairs",
+                                              "axes")] + [("norm_eps", ctypes.c_float), ("rot_gain", ctypes.c_float)]
+
+    @classmethod
+    def make(cls, B, H, Hkv, d, rows=1, rot=None, pairs=HALVES, axes=1, eps=1e-6, gain=0.0):
+        return cls(B, H, Hkv, d, rows, d if rot is None else rot, pairs, axes, float(eps), float(gain))
+
+    def __repr__(self):
+        return (f"Heads(B={self.batch}, H={self.n_heads}, Hkv={self.n_kv_heads}, d={self.head_dim}, rows={self.rows}, "
+                f"rot={self.rot_dim}, pairs={'neighbours' if self.pairs == NEIGHBOURS else 'halves'}, axes={self.axes})")
+
+
+class _Rows(ctypes.Structure):
+    """Mirror of ``ugbs_rows``."""
+    _fields_ = [("at", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -144,11 +165,14 @@ def lib():
         L.ugbs_cache_attend.argtypes = [pc] + 8 * [P] + [ctypes.c_size_t, P]
         L.ugbs_cache_workspace_bytes.argtypes = [pc]
         L.ugbs_cache_workspace_bytes.restype = ctypes.c_size_t
+        ph, pr = ctypes.POINTER(Heads), ctypes.POINTER(_Rows)
+        L.ugbs_heads_split.argtypes = [ph, pr, pr, pr] + 11 * [P]
+        L.ugbs_heads_store.argtypes = [ph, pc, pr, pr, pr] + 12 * [P]
         for f in ("ugbs_block_meta", "ugbs_score_select", "ugbs_route", "ugbs_attend", "ugbs_abi_version",
                   "ugbs_attend_select", "ugbs_select_rows", "ugbs_attend_bitmap",
                   "ugbs_noise_scale", "ugbs_bai_tiles", "ugbs_bai_heads", "ugbs_route_noalloc",
                   "ugbs_quest_scores_valu", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
-                  "ugbs_cache_attend"):
+                  "ugbs_cache_attend", "ugbs_heads_split", "ugbs_heads_store"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -172,14 +196,14 @@ def ugbs_workspace_bytes(p: Problem) -> int:
 # for as a raw handle, and a call's sizes are read from the problem once.
 
 _torch = None
-_BF16 = _I32 = _F32 = ()
+_BF16 = _I32 = _F32 = _F64 = ()
 _raw_stream = None
 
 
 def _load_torch():
-    global _torch, _BF16, _I32, _F32, _raw_stream
+    global _torch, _BF16, _I32, _F32, _F64, _raw_stream
     import torch
-    _I32, _F32 = (torch.int32,), (torch.float32,)
+    _I32, _F32, _F64 = (torch.int32,), (torch.float32,), (torch.float64,)
     _BF16 = (torch.bfloat16, torch.int16, torch.uint16)
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
     _torch = torch
@@ -567,6 +591,66 @@ def ugbs_cache_attend(c: Cache, Q, cache, scales, table, kv_lens, q_lens, O, wor
           *_cache_arrays(c, cache, scales, c.n_pages, c.n_kv_heads, d, x, dev),
           _addr("table", table, (B, c.max_pages), _I32, x, dev), _addr("kv_lens", kv_lens, one, _I32, x, dev),
           _addr("q_lens", q_lens, one, _I32, x, dev), _addr("O", O, shape, _BF16, x, dev), ws, nbytes)
+
+
+# ---------------------------------------------------------------- heads
+
+def _rows_of(name, t, shape, index, dev):
+    """A tensor [B,rows,heads,d] whose last axis is contiguous, by its strides."""
+    if t is None:
+        raise ValueError(f"{name} is required")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)} != expected {tuple(shape)}")
+    if t.dtype not in _BF16:
+        raise ValueError(f"{name}: dtype {t.dtype} not in {_BF16}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+    b, i, h, c = t.stride()
+    if c != 1:
+        raise ValueError(f"{name}: the channels of a head must follow each other")
+    # (the stride of an axis of one is anything)
+    return _Rows(t.data_ptr(), b if shape[0] > 1 else 0, i if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
+
+
+def _maybe(name, t, shape, dtypes, index, dev):
+    return None if t is None else _addr(name, t, shape, dtypes, index, dev)
+
+
+def _heads_args(h, Xq, Xk, Xv, freqs, q_norm, k_norm, positions, axis, first, lens, index, dev):
+    B, H, Hkv, d, rows = h.batch, h.n_heads, h.n_kv_heads, h.head_dim, h.rows
+    kv, w, half = (B, rows, Hkv, d), (d,), (h.rot_dim // 2,)
+    return (ctypes.byref(_rows_of("Xq", Xq, (B, rows, H, d), index, dev)), ctypes.byref(_rows_of("Xk", Xk, kv, index, dev)),
+            ctypes.byref(_rows_of("Xv", Xv, kv, index, dev)), _maybe("q_norm", q_norm, w, _F32, index, dev),
+            _maybe("k_norm", k_norm, w, _F32, index, dev), _maybe("freqs", freqs, half, _F64, index, dev),
+            _maybe("positions", positions, (h.axes, B, rows), _I32, index, dev), _maybe("axis", axis, half, _I32, index, dev),
+            _maybe("first", first, (B,), _I32, index, dev), _maybe("lens", lens, (B,), _I32, index, dev))
+
+
+def ugbs_heads_split(h: Heads, Xq, Xk, Xv, freqs, Q, K, V, q_norm=None, k_norm=None, positions=None, axis=None, first=None,
+                     lens=None, stream=None):
+    """A projection's rows Xq [B,rows,H,d], Xk, Xv [B,rows,Hkv,d] bf16 (any strides: views of a packed projection) ->
+    Q [B,H,rows,d], K, V [B,Hkv,rows,d] bf16: queries and keys normed per head (with a weight [d] fp32) and rotated
+    by position * freqs ([rot/2] fp64).  Positions: [axes,B,rows] int32, pair j by axis[j] ([rot/2] int32); or first[b] + i.
+    Rows behind lens[b] are neither read nor written."""
+    _get_torch()
+    x, dev = _device_of("Xq", Xq)
+    B, rows, d = h.batch, h.rows, h.head_dim
+    kv = (B, h.n_kv_heads, rows, d)
+    _call("ugbs_heads_split", x, stream, h,
+          *_heads_args(h, Xq, Xk, Xv, freqs, q_norm, k_norm, positions, axis, first, lens, x, dev),
+          _addr("Q", Q, (B, h.n_heads, rows, d), _BF16, x, dev), _addr("K", K, kv, _BF16, x, dev), _addr("V", V, kv, _BF16, x, dev))
+
+
+def ugbs_heads_store(h: Heads, c: Cache, Xq, Xk, Xv, freqs, Q, slots, cache, scales, q_norm=None, k_norm=None, positions=None,
+                     axis=None, first=None, lens=None, stream=None):
+    """ugbs_heads_split's Q, and its K and V straight into the cache as ugbs_cache_store puts them there."""
+    _get_torch()
+    x, dev = _device_of("Xq", Xq)
+    B, rows, d = h.batch, h.rows, h.head_dim
+    _call("ugbs_heads_store", x, stream, h, ctypes.byref(c),
+          *_heads_args(h, Xq, Xk, Xv, freqs, q_norm, k_norm, positions, axis, first, lens, x, dev),
+          _addr("Q", Q, (B, h.n_heads, rows, d), _BF16, x, dev), _addr("slots", slots, (B, c.rows), _I32, x, dev),
+          *_cache_arrays(c, cache, scales, c.n_pages, c.n_kv_heads, d, x, dev))
 
 
 # ---------------------------------------------------------------- convenience

@@ -80,6 +80,8 @@ const char* ugbs_status_string(int status) {
     case UGBS_ERR_SCRATCH: return "problem exceeds the static scratch of ugbs_route_noalloc";
     case UGBS_ERR_DTYPE: return "unknown cache type";
     case UGBS_ERR_ALIAS: return "an output is one of the call's other arrays";
+    case UGBS_ERR_ROTARY: return "invalid rot_dim, pairs, axes, norm_eps or rot_gain";
+    case UGBS_ERR_STRIDE: return "a stride is not a multiple of 8";
     default: return "unknown status";
   }
 }

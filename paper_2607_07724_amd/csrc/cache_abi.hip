@@ -1,40 +1,15 @@
 // extern "C" boundary of the cache's entry points: argument validation, derived
 // sizes and dispatch.  Every check runs before anything is enqueued; nothing here
 // allocates, frees or synchronises.
-#include <cmath>
-
-#include "cache_internal.h"
+#include "cache_check.h"
 
 namespace {
 
 using ugbs::CacheShape;
+using ugbs::make_cache;
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 int hip_status(hipError_t e) { return e == hipSuccess ? UGBS_OK : UGBS_ERR_HIP; }
-
-// Workgroups that touch n consecutive tokens' pages, of up to 512 threads: a grid holds 2^32 threads.
-bool grid_fits(int64_t batch_heads, int64_t n) { return batch_heads * ((n + 62) / 64 + 1) <= (1 << 22); }
-
-int make_cache(const ugbs_cache* c, CacheShape* s) {
-  if (!c) return UGBS_ERR_NULL;
-  if (c->batch < 1 || c->batch > UGBS_MAX_REQUESTS) return UGBS_ERR_SHAPE;
-  if (c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads) return UGBS_ERR_SHAPE;
-  if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return UGBS_ERR_SHAPE;
-  if (c->n_pages < 1 || c->n_pages > UGBS_MAX_PAGES) return UGBS_ERR_SHAPE;
-  if (c->max_pages < 1 || c->max_pages > UGBS_MAX_BLOCKS) return UGBS_ERR_SHAPE;
-  if (c->rows < 1 || c->rows > c->max_pages * UGBS_BLOCK) return UGBS_ERR_SHAPE;
-  if (c->dtype != UGBS_E4M3 && c->dtype != UGBS_INT8) return UGBS_ERR_DTYPE;
-  if (!std::isfinite(c->softmax_scale) || c->softmax_scale < 0.0f) return UGBS_ERR_SCALE;
-  const int G = c->n_heads / c->n_kv_heads;
-  // grids of the kernels (tiles of 16 rows, 256 threads), and slots counted with 32 bits
-  const int64_t heads = (int64_t)c->batch * c->n_kv_heads;
-  if (heads > (1 << 22) || !grid_fits(heads, c->rows)) return UGBS_ERR_SHAPE;
-  if ((int64_t)c->rows * G > (1 << 30) || heads * (((int64_t)c->rows * G + 15) / 16) > (1 << 23)) return UGBS_ERR_SHAPE;
-  if ((int64_t)c->batch * c->rows > (1 << 30)) return UGBS_ERR_SHAPE;
-  *s = CacheShape{c->batch, c->n_heads, c->n_kv_heads, G, c->head_dim, c->n_pages, c->max_pages, c->rows, c->dtype,
-                  c->softmax_scale > 0.0f ? c->softmax_scale : 1.0f / std::sqrt((float)c->head_dim)};
-  return UGBS_OK;
-}
 
 }  // namespace
 
@@ -89,7 +64,7 @@ int ugbs_cache_load(const ugbs_cache* c, const void* cache, const float* scales,
   const int st = make_cache(c, &s);
   if (st) return st;
   if (!cache || !scales || !table || !start || !count || !K || !V) return UGBS_ERR_NULL;
-  if (width < 1 || width > UGBS_MAX_WIDTH || !grid_fits((int64_t)s.B * s.Hkv, width)) return UGBS_ERR_SHAPE;
+  if (width < 1 || width > UGBS_MAX_WIDTH || !ugbs::grid_fits((int64_t)s.B * s.Hkv, width)) return UGBS_ERR_SHAPE;
   if (!aligned(K, 16) || !aligned(V, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(table, 4) ||
       !aligned(start, 4) || !aligned(count, 4))
     return UGBS_ERR_ALIGN;

@@ -1,0 +1,222 @@
+// From a projection's rows to heads: the norm of a query or key head, its rotation by
+// position, and the launchers of the kernels.
+//
+// A row is the d channels of one head of one token.  d / 16 lanes hold it, 16 channels
+// each, as two eights A and B: of the rotated channels those that the rotation pairs
+// (8 l .. 8 l + 7 with rot / 2 + 8 l .., or 16 neighbours), so a lane rotates by itself with
+// 8 angles, 8 l .. 8 l + 7; of the others 16 in a row.
+//   y = x / sqrt(mean x^2 + eps) * w,   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
+// in fp32, rounded to bf16 once at the end.  Products and sums are written as the
+// operations they are (no contraction left to the compiler), so that every kernel that
+// takes a row gives the same bits.
+#pragma once
+#include "cache_internal.h"
+
+namespace ugbs {
+
+struct HeadsShape {
+  int B, H, Hkv, d, rows, rot, pairs, axes;
+  float eps, gain;
+};
+
+struct HeadsParams {
+  HeadsShape s;
+  ugbs_rows q, k, v;
+  const float* q_norm;
+  const float* k_norm;
+  const double* freqs;
+  const int32_t* axis;
+  const int32_t* positions;
+  const int32_t* first;
+  const int32_t* lens;
+  uint16_t* Q;
+  uint16_t* K;
+  uint16_t* V;
+};
+
+hipError_t launch_heads_split(const HeadsParams& P, hipStream_t stream);
+hipError_t launch_heads_store(const HeadsParams& P, const CacheShape& c, const int32_t* slots, uint8_t* cache, float* scales,
+                              hipStream_t stream);
+
+namespace {
+
+// (cos, sin) of 2 pi t times gain.  t modulo a quarter turn in 64 bits leaves |y| <= 1/8;
+// cos and sin of 2 pi y by their Taylor series, which end 1e-10 and 2e-9 off at an eighth.
+__device__ __forceinline__ float2 turned(double t, float gain) {
+  const double quarters = __builtin_rint(4.0 * t);
+  const float x = (float)(__builtin_fma(-0.25, quarters, t) * 6.283185307179586);
+  // quarters mod 4 (of numbers up to 2^33, exact)
+  const int n = (int)__builtin_fma(-4.0, __builtin_floor(0.25 * quarters), quarters);
+  const float z = x * x;
+  float s = __builtin_fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
+  s = __builtin_fmaf(z, s, 8.3333333e-3f);
+  s = __builtin_fmaf(z, s, -1.6666667e-1f);
+  s = __builtin_fmaf(z * x, s, x);
+  float c = __builtin_fmaf(z, -2.7557319e-7f, 2.4801587e-5f);
+  c = __builtin_fmaf(z, c, -1.3888889e-3f);
+  c = __builtin_fmaf(z, c, 4.1666667e-2f);
+  c = __builtin_fmaf(z, c, -0.5f);
+  c = __builtin_fmaf(z, c, 1.0f);
+  const float a = n & 1 ? s : c, b = n & 1 ? c : s;
+  return make_float2((n == 1 || n == 2 ? -a : a) * gain, (n >= 2 ? -b : b) * gain);
+}
+
+// The angle of pair j at token i of request b.
+__device__ __forceinline__ float2 angle_of(const HeadsParams& P, int b, int i, int j) {
+  int pos;
+  if (P.positions) {
+    const int a = P.axis ? min(max(P.axis[j], 0), P.s.axes - 1) : 0;
+    pos = P.positions[((size_t)a * P.s.B + b) * P.s.rows + i];
+    return turned((double)pos * (P.freqs[j] * 0.15915494309189535), P.s.gain);
+  }
+  const int64_t at = (int64_t)(P.first ? P.first[b] : 0) + i;
+  return turned((double)at * (P.freqs[j] * 0.15915494309189535), P.s.gain);
+}
+
+__device__ __forceinline__ int rows_of(const HeadsParams& P, int b) {
+  return P.lens ? min(max(P.lens[b], 0), P.s.rows) : P.s.rows;
+}
+
+// Where the eights of lane l of a row lie.
+template <int PAIRS>
+__device__ __forceinline__ int2 eights_of(const HeadsShape& s, int l) {
+  if (PAIRS == UGBS_HALVES && 16 * l < s.rot) return make_int2(8 * l, s.rot / 2 + 8 * l);
+  return make_int2(16 * l, 16 * l + 8);
+}
+
+// Sum over the LANES lanes of a row (4, 8 or 16, all active).
+template <int LANES>
+__device__ __forceinline__ float sum_row(float x) {
+  auto add = [&](int y) { x += __uint_as_float((unsigned)y); };
+  add(dpp<0xb1, 0xf>((int)__float_as_uint(x)));                       // lane ^ 1
+  add(dpp<0x4e, 0xf>((int)__float_as_uint(x)));                       // lane ^ 2
+  if (LANES >= 8) add(dpp<0x141, 0xf>((int)__float_as_uint(x)));      // 7 - lane, within 8
+  if (LANES >= 16) add(dpp<0x140, 0xf>((int)__float_as_uint(x)));     // 15 - lane, within 16
+  return x;
+}
+
+__device__ __forceinline__ void unpack8(uint4 v, float* x) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    x[2 * e] = __uint_as_float(w[e] << 16);
+    x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ uint4 pack8(const float* x) {
+  return make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
+// One row: this lane's eights a, b.  w: their 16 weights (NORM).  All lanes of the row are active.
+template <int D, int PAIRS, bool NORM>
+__device__ __forceinline__ void do_row(uint4& a, uint4& b, const float (&w)[16], const float2 (&cs)[8], bool rotated, float eps) {
+  float x[16];
+  unpack8(a, x);
+  unpack8(b, x + 8);
+  if constexpr (NORM) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) sum = __builtin_fmaf(x[e], x[e], sum);
+    sum = sum_row<D / 16>(sum);
+    const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, 1.0f / D, eps));
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = x[e] * r * w[e];
+  }
+  if (rotated) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      constexpr bool H = PAIRS == UGBS_HALVES;
+      const int p = H ? j : 2 * j, q = H ? j + 8 : 2 * j + 1;
+      const float u = x[p], v = x[q];
+      x[p] = __builtin_fmaf(u, cs[j].x, -(v * cs[j].y));
+      x[q] = __builtin_fmaf(v, cs[j].x, u * cs[j].y);
+    }
+  }
+  a = pack8(x);
+  b = pack8(x + 8);
+}
+
+__device__ __forceinline__ void weights_of(const float* norm, int2 c, float (&w)[16]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float4 y = *reinterpret_cast<const float4*>(norm + (e < 2 ? c.x : c.y) + 4 * (e & 1));
+    w[4 * e] = y.x;
+    w[4 * e + 1] = y.y;
+    w[4 * e + 2] = y.z;
+    w[4 * e + 3] = y.w;
+  }
+}
+
+__device__ __forceinline__ const uint16_t* row_at(const ugbs_rows& r, int b, int i, int h) {
+  return static_cast<const uint16_t*>(r.at) + b * r.batch + i * r.token + h * r.head;
+}
+
+// Tokens of a wave: 1024 / d rows of one head at a time.
+template <int D>
+constexpr int kTokens = 1024 / D;
+
+// Heads h0 .. h1 - 1 of the queries, keys and values, in this order, of tokens n0 .. of the batch:
+// the work of a workgroup of NW waves.  A wave takes a head of kTokens tokens at a time, whose
+// rows follow each other in the result (1 to 2 KiB in a row).  The angles are formed once, in LDS,
+// and stay in registers over the heads.
+template <int D, int PAIRS, int NW>
+__device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0, int h1, float2* s_angle) {
+  constexpr int LANES = D / 16, T = kTokens<D>;
+  const HeadsShape& s = P.s;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l = lane % LANES, total = s.B * s.rows, half = s.rot / 2;
+  const int n = min(n0 + lane / LANES, total - 1), b = n / s.rows, i = n % s.rows;
+  const bool live = n0 + lane / LANES < total && i < rows_of(P, b), rotated = 16 * l < s.rot;
+  float2 cs[8];
+  if (s.rot > 0 && h0 < s.H + s.Hkv) {
+    for (int x = tid; x < T * half; x += 64 * NW) {
+      const int t = min(n0 + x / half, total - 1);
+      s_angle[x] = angle_of(P, t / s.rows, t % s.rows, x % half);
+    }
+    __syncthreads();
+    const float4* const from = reinterpret_cast<const float4*>(s_angle + lane / LANES * half + (rotated ? 8 * l : 0));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float4 y = from[e];
+      cs[2 * e] = make_float2(y.x, y.y);
+      cs[2 * e + 1] = make_float2(y.z, y.w);
+    }
+  }
+  const int2 c = eights_of<PAIRS>(s, l);
+  int h = h0 + w;
+  auto part = [&](const ugbs_rows& from, uint16_t* to, const float* norm, int before, int heads, bool turn) {
+    if (h >= min(h1, before + heads)) return;
+    float wt[16];
+    if (norm) weights_of(norm, c, wt);
+    const uint16_t* const x = row_at(from, b, i, 0);
+    uint16_t* const y = to + ((size_t)b * heads * s.rows + i) * D;
+    for (; h < min(h1, before + heads); h += NW) {
+      uint4 u = make_uint4(0, 0, 0, 0), v = u;
+      if (live) {
+        const uint16_t* const at = x + (int64_t)(h - before) * from.head;
+        u = *reinterpret_cast<const uint4*>(at + c.x);
+        v = *reinterpret_cast<const uint4*>(at + c.y);
+      }
+      if (norm) do_row<D, PAIRS, true>(u, v, wt, cs, turn && rotated, s.eps);
+      else if (turn) do_row<D, PAIRS, false>(u, v, wt, cs, rotated, s.eps);
+      if (live) {
+        uint16_t* const at = y + (size_t)(h - before) * s.rows * D;
+        *reinterpret_cast<uint4*>(at + c.x) = u;
+        *reinterpret_cast<uint4*>(at + c.y) = v;
+      }
+    }
+  };
+  part(P.q, P.Q, P.q_norm, 0, s.H, s.rot > 0);
+  if (h1 <= s.H) return;
+  part(P.k, P.K, P.k_norm, s.H, s.Hkv, s.rot > 0);
+  part(P.v, P.V, nullptr, s.H + s.Hkv, s.Hkv, false);
+}
+
+// Workgroups along the heads: one head a wave where tokens are few.
+inline int head_slices(int64_t groups, int heads, int waves) {
+  const int64_t most = (heads + waves - 1) / waves, want = (1024 + groups - 1) / groups;
+  return (int)(want < most ? want : most);
+}
+
+}  // namespace
+}  // namespace ugbs
