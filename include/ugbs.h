@@ -26,6 +26,7 @@
  *   ugbs_attend_bitmap(Q, K, V, bitmap)      -> O
  * and, for the tokens after the prompt, a paged cache in 8 bits:
  *   ugbs_cache_plan, ugbs_cache_store, ugbs_cache_attend, ugbs_cache_load
+ *   (with common first pages: ugbs_cache_share, ugbs_cache_attend_shared)
  * Before them, from a projection's rows (norms of heads, rotation by position):
  *   ugbs_heads_split  (rows)                 -> Q, K, V
  *   ugbs_heads_store  (rows, slots)          -> Q, cache
@@ -563,6 +564,37 @@ UGBS_API int ugbs_cache_attend(const ugbs_cache* c, const void* Q, const void* c
 
 /* Bytes of device workspace of ugbs_cache_attend (0 if c is invalid). */
 UGBS_API size_t ugbs_cache_workspace_bytes(const ugbs_cache* c);
+
+/* Attention of a batch whose requests list common first pages (a system prompt, several
+ * answers to one prompt): each common page is read once for all rows of a group instead of
+ * once for each request.  The result is that of ugbs_cache_attend but for the order of sums.
+ *
+ * ugbs_cache_share lays a step out, once for all its layers, after ugbs_cache_plan:
+ *   group   : [B] int32: requests of equal numbers >= 0 are a group; negative: alone.  What a
+ *             group shares are the first entries that the table rows of all its requests
+ *             with new tokens have in common, as far as these pages are full for all of them.
+ *             Requests that turn out to have nothing in common cost nothing, and no answer depends on group.
+ *   table, kv_lens, q_lens : the step's.
+ *   share   : device memory of at least ugbs_cache_share_bytes(c) bytes, 256-byte aligned,
+ *             contents ignored; holds the layout until the next call. */
+UGBS_API int ugbs_cache_share(const ugbs_cache* c, const int32_t* group, const int32_t* table, const int32_t* kv_lens,
+                              const int32_t* q_lens, void* share, size_t share_bytes, void* stream);
+
+/* ugbs_cache_attend over a layout.
+ *   table, kv_lens, q_lens, share : those of the ugbs_cache_share call, which comes before on the stream.
+ *   workspace : at least ugbs_cache_shared_workspace_bytes(c) bytes, else as for ugbs_cache_attend.
+ *   For common pages the rows of all requests count together, batch rows H / H_kv, where
+ *   ugbs_cache_attend takes a query channel as two e4m3 numbers.
+ *   Where rows H / H_kv > 64 (pieces of prompts), each request's rows fill tiles of their own,
+ *   bound by the matrix cores; there, with one request and with batch rows H > 2^20 nothing is
+ *   shared and the call is ugbs_cache_attend. */
+UGBS_API int ugbs_cache_attend_shared(const ugbs_cache* c, const void* Q, const void* cache, const float* scales,
+                                      const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, const void* share,
+                                      size_t share_bytes, void* O, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of a layout, and of device workspace of ugbs_cache_attend_shared (0 if c is invalid). */
+UGBS_API size_t ugbs_cache_share_bytes(const ugbs_cache* c);
+UGBS_API size_t ugbs_cache_shared_workspace_bytes(const ugbs_cache* c);
 
 /* ---- From a projection's rows to heads -----------------------------------------
  * A projection gives a token's queries, keys and values next to each other; the

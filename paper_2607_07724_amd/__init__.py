@@ -27,6 +27,7 @@ __all__ = [
     "E4M3", "INT8", "CACHE_RELEASE", "Cache", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
     "ugbs_cache_attend", "ugbs_cache_workspace_bytes", "CacheBuffers", "CacheStep", "prefill_cached", "cache_layer",
     "HALVES", "NEIGHBOURS", "Heads", "ugbs_heads_split", "ugbs_heads_store",
+    "ugbs_cache_share", "ugbs_cache_attend_shared", "ugbs_cache_share_bytes", "ugbs_cache_shared_workspace_bytes",
 ]
 
 KMEAN, QUEST = 0, 1
@@ -165,6 +166,11 @@ def lib():
         L.ugbs_cache_attend.argtypes = [pc] + 8 * [P] + [ctypes.c_size_t, P]
         L.ugbs_cache_workspace_bytes.argtypes = [pc]
         L.ugbs_cache_workspace_bytes.restype = ctypes.c_size_t
+        L.ugbs_cache_share.argtypes = [pc] + 5 * [P] + [ctypes.c_size_t, P]
+        L.ugbs_cache_attend_shared.argtypes = [pc] + 7 * [P] + [ctypes.c_size_t, P, P, ctypes.c_size_t, P]
+        for f in ("ugbs_cache_share_bytes", "ugbs_cache_shared_workspace_bytes"):
+            getattr(L, f).argtypes = [pc]
+            getattr(L, f).restype = ctypes.c_size_t
         ph, pr = ctypes.POINTER(Heads), ctypes.POINTER(_Rows)
         L.ugbs_heads_split.argtypes = [ph, pr, pr, pr] + 11 * [P]
         L.ugbs_heads_store.argtypes = [ph, pc, pr, pr, pr] + 12 * [P]
@@ -172,7 +178,8 @@ def lib():
                   "ugbs_attend_select", "ugbs_select_rows", "ugbs_attend_bitmap",
                   "ugbs_noise_scale", "ugbs_bai_tiles", "ugbs_bai_heads", "ugbs_route_noalloc",
                   "ugbs_quest_scores_valu", "ugbs_cache_plan", "ugbs_cache_store", "ugbs_cache_load",
-                  "ugbs_cache_attend", "ugbs_heads_split", "ugbs_heads_store"):
+                  "ugbs_cache_attend", "ugbs_heads_split", "ugbs_heads_store", "ugbs_cache_share",
+                  "ugbs_cache_attend_shared"):
             getattr(L, f).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -591,6 +598,44 @@ def ugbs_cache_attend(c: Cache, Q, cache, scales, table, kv_lens, q_lens, O, wor
           *_cache_arrays(c, cache, scales, c.n_pages, c.n_kv_heads, d, x, dev),
           _addr("table", table, (B, c.max_pages), _I32, x, dev), _addr("kv_lens", kv_lens, one, _I32, x, dev),
           _addr("q_lens", q_lens, one, _I32, x, dev), _addr("O", O, shape, _BF16, x, dev), ws, nbytes)
+
+
+def ugbs_cache_share_bytes(c: Cache) -> int:
+    return int(lib().ugbs_cache_share_bytes(ctypes.byref(c)))
+
+
+def ugbs_cache_shared_workspace_bytes(c: Cache) -> int:
+    return int(lib().ugbs_cache_shared_workspace_bytes(ctypes.byref(c)))
+
+
+def _buffer(name, t, index, dev):
+    """Address and bytes of device memory of any shape and type."""
+    return (None, 0) if t is None else (_addr(name, t, t.shape, (t.dtype,), index, dev), t.nbytes)
+
+
+def ugbs_cache_share(c: Cache, group, table, kv_lens, q_lens, share, stream=None):
+    """The layout of a step for ugbs_cache_attend_shared, into `share` (>= ugbs_cache_share_bytes(c) bytes): requests of
+    equal group [B] int32 (>= 0) share the first pages that their table rows have in common."""
+    _get_torch()
+    x, dev = _device_of("group", group)
+    one = (c.batch,)
+    _call("ugbs_cache_share", x, stream, c, _addr("group", group, one, _I32, x, dev),
+          _addr("table", table, (c.batch, c.max_pages), _I32, x, dev), _addr("kv_lens", kv_lens, one, _I32, x, dev),
+          _addr("q_lens", q_lens, one, _I32, x, dev), *_buffer("share", share, x, dev))
+
+
+def ugbs_cache_attend_shared(c: Cache, Q, cache, scales, table, kv_lens, q_lens, share, O, workspace=None, stream=None):
+    """ugbs_cache_attend with the pages that requests have in common read once, by the layout `share` of this step's
+    ugbs_cache_share; workspace: >= ugbs_cache_shared_workspace_bytes(c) bytes."""
+    _get_torch()
+    x, dev = _device_of("Q", Q)
+    B, d = c.batch, c.head_dim
+    shape, one = (B, c.n_heads, c.rows, d), (B,)
+    _call("ugbs_cache_attend_shared", x, stream, c, _addr("Q", Q, shape, _BF16, x, dev),
+          *_cache_arrays(c, cache, scales, c.n_pages, c.n_kv_heads, d, x, dev),
+          _addr("table", table, (B, c.max_pages), _I32, x, dev), _addr("kv_lens", kv_lens, one, _I32, x, dev),
+          _addr("q_lens", q_lens, one, _I32, x, dev), *_buffer("share", share, x, dev), _addr("O", O, shape, _BF16, x, dev),
+          *_buffer("workspace", workspace, x, dev))
 
 
 # ---------------------------------------------------------------- heads

@@ -32,7 +32,7 @@ ARCH = "gfx950"
 LLVM_BIN = "/opt/rocm/lib/llvm/bin"
 
 SOURCES = ["block_meta.hip", "score_select.hip", "route.hip", "attend.hip", "attend_keys.hip", "rowsel.hip", "bai.hip", "quest_valu.hip", "abi.hip",
-           "cache_plan.hip", "cache_store.hip", "cache_attend.hip", "cache_tiles.hip", "cache_abi.hip",
+           "cache_plan.hip", "cache_store.hip", "cache_attend.hip", "cache_tiles.hip", "cache_share.hip", "cache_abi.hip",
            "heads.hip", "heads_store.hip", "heads_abi.hip"]
 PROBE_SOURCES = ["probe_peaks.hip"]
 

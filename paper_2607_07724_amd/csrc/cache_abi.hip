@@ -90,4 +90,44 @@ int ugbs_cache_attend(const ugbs_cache* c, const void* Q, const void* cache, con
                                               static_cast<hipStream_t>(stream)));
 }
 
+size_t ugbs_cache_share_bytes(const ugbs_cache* c) {
+  CacheShape s;
+  return make_cache(c, &s) == UGBS_OK ? ugbs::cache_share_bytes(s) : 0;
+}
+
+size_t ugbs_cache_shared_workspace_bytes(const ugbs_cache* c) {
+  CacheShape s;
+  return make_cache(c, &s) == UGBS_OK ? ugbs::cache_shared_workspace(s) : 0;
+}
+
+int ugbs_cache_share(const ugbs_cache* c, const int32_t* group, const int32_t* table, const int32_t* kv_lens,
+                     const int32_t* q_lens, void* share, size_t share_bytes, void* stream) {
+  CacheShape s;
+  const int st = make_cache(c, &s);
+  if (st) return st;
+  if (!group || !table || !kv_lens || !q_lens) return UGBS_ERR_NULL;
+  if (!share || share_bytes < ugbs::cache_share_bytes(s)) return UGBS_ERR_WORKSPACE;
+  if (!aligned(group, 4) || !aligned(table, 4) || !aligned(kv_lens, 4) || !aligned(q_lens, 4) || !aligned(share, 256))
+    return UGBS_ERR_ALIGN;
+  return hip_status(ugbs::launch_cache_share(s, group, table, kv_lens, q_lens, share, static_cast<hipStream_t>(stream)));
+}
+
+int ugbs_cache_attend_shared(const ugbs_cache* c, const void* Q, const void* cache, const float* scales, const int32_t* table,
+                             const int32_t* kv_lens, const int32_t* q_lens, const void* share, size_t share_bytes, void* O,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  CacheShape s;
+  const int st = make_cache(c, &s);
+  if (st) return st;
+  if (!Q || !cache || !scales || !table || !kv_lens || !q_lens || !O) return UGBS_ERR_NULL;
+  const size_t need = ugbs::cache_shared_workspace(s);
+  if (need > 0 && (!workspace || workspace_bytes < need)) return UGBS_ERR_WORKSPACE;
+  if (!share || share_bytes < ugbs::cache_share_bytes(s)) return UGBS_ERR_WORKSPACE;
+  if (!aligned(Q, 16) || !aligned(O, 16) || !aligned(cache, 16) || !aligned(scales, 8) || !aligned(table, 4) ||
+      !aligned(kv_lens, 4) || !aligned(q_lens, 4) || !aligned(share, 256) || (need > 0 && !aligned(workspace, 256)))
+    return UGBS_ERR_ALIGN;
+  return hip_status(ugbs::launch_cache_attend_shared(s, static_cast<const uint16_t*>(Q), static_cast<const uint8_t*>(cache),
+                                                     scales, table, kv_lens, q_lens, share, static_cast<uint16_t*>(O), workspace,
+                                                     static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

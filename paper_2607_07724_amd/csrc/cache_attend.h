@@ -27,6 +27,22 @@ struct Schedule {
   int2* long_tile;    // [kLongTiles]: request (-1 behind the last), which of its tiles
 };
 
+// Where the parts lie of a batch whose requests list common first pages: formed once a step by
+// ugbs_cache_share.  A group of such requests has a leader, its first one.  The rows of a part's sums
+// lie in the workspace one behind another, a tile's rows rounded up to 16: part `split` of tile t, kv
+// head h of rows R in all (R a multiple of 16) begins at row
+//   before + splits (h R + t ROWS) + split min(ROWS, R - t ROWS).
+struct Share {
+  int4* own;          // [B][3]: (parts before, parts of a tile, rows before or -1: written to O, the first page that is its own),
+                      //   (rows before of its group's prefix or -1, parts of a tile there, first new token in the group, group's R),
+                      //   (new tokens, cached tokens, -, -)
+  int4* prefix;       // [B][2], of leaders: (parts before, parts of a tile, rows before, first entry in `row`), (new tokens, pages, -, -)
+  int32_t* own_part;  // [own_parts]: the request, -1 behind the last part
+  int32_t* prefix_part;   // [prefix_parts]: the leader, -1 behind the last part
+  int2* row;          // [B rows]: new tokens of the groups: request * rows + token, the last key it sees
+  int4* found;        // [B]: leader (-1: alone), pages in common with it, new tokens of the group's requests before
+};
+
 struct CacheAttendParams {
   CacheShape s;
   const uint16_t* Q;
@@ -42,10 +58,18 @@ struct CacheAttendParams {
   bool splits;        // parts are allowed
   Schedule schedule;  // of more than kWaveBatch requests
   int min_pages;
+  Share share;        // of common first pages
 };
+
+// What a launch of the parts takes: whole requests; the pages that are a request's own, those that groups
+// have in common (ugbs_cache_attend_shared).
+enum Mode { kWhole, kOwn, kPrefix };
 
 // Tiles of 64 (d 256: 32) rows, where rows are many (cache_tiles.hip).
 hipError_t launch_cache_tiles(const CacheAttendParams& P, hipStream_t stream);
+void launch_shared_tiles(const CacheAttendParams& P, Mode mode, unsigned parts, bool once, hipStream_t stream);
+// Tiles of 16 or 32 rows (cache_attend.hip).
+void launch_shared_rows(const CacheAttendParams& P, Mode mode, unsigned parts, int rows_of_a_tile, hipStream_t stream);
 constexpr int tile_rows_many(int d) { return d == 256 ? 32 : 64; }
 
 namespace {
@@ -95,10 +119,9 @@ struct Part {
 // three quarters of the tiles are taken off (56 tiles: as 560 parts 264 us, as 504 193).  Tiles
 // of a few pages among long ones end no part that matters and are not counted (one request
 // of 100K among 3 of 100, 64 rows of 64/16 heads, d 64: 220 -> 156 us).
-template <int ROWS>
-__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, float work, float tiles, float wide) {
+__device__ __forceinline__ int pages_per_part(const CacheAttendParams& P, int rows, float work, float tiles, float wide) {
   if (!P.splits) return UGBS_MAX_BLOCKS;
-  const float off = (ROWS <= 32 ? 0.5f : 0.75f) * wide * (float)P.s.Hkv;
+  const float off = (rows <= 32 ? 0.5f : 0.75f) * wide * (float)P.s.Hkv;
   const float aim = fmaxf((float)kTarget - off, 0.5f * kTarget);
   const float x = work * (float)P.s.Hkv / aim;
   // (256 tiles fill the chip: 512 tokens attending to themselves 26 us split, 20 whole)
@@ -180,7 +203,7 @@ __device__ bool find_part(const CacheAttendParams& P, int pos, Part* out) {
 #pragma unroll
   for (int k = 0; k < NC; ++k)
     if (is_wide(P, r[k], work)) wide += (float)r[k].tiles;
-  const int per = __builtin_amdgcn_readfirstlane(pages_per_part<ROWS>(P, work, sum_wave(tiles), sum_wave(wide)));
+  const int per = __builtin_amdgcn_readfirstlane(pages_per_part(P, ROWS, work, sum_wave(tiles), sum_wave(wide)));
   int before = 0, slots = 0;
 #pragma unroll
   for (int k = 0; k < NC; ++k) {
@@ -252,7 +275,7 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
   wide = 0.f;
 #pragma unroll
   for (int v = 0; v < NW; ++v) wide += s_wide[v];
-  const int per = pages_per_part<ROWS>(P, work, tiles, wide);
+  const int per = pages_per_part(P, ROWS, work, tiles, wide);
   int n[4] = {0, 0, 0, 0};                  // parts, slots, split tiles, long tiles
   int splits[PER];
 #pragma unroll
@@ -314,6 +337,35 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
     P.schedule.part[i] = i < total[0] ? request_at(s_parts, i) : -1;
   if (blockIdx.x == 0 && tid >= total[3] && tid < kLongTiles) P.schedule.long_tile[tid] = make_int2(-1, 0);
   if (blockIdx.x == 0 && tid < kTarget) P.schedule.join[tid] = tid < total[2] ? request_at(s_joins, tid) : -1;
+}
+
+// A part of a shared batch; *row: where its sums go, -1: it is its rows' only one.  *first: its first page.
+template <int ROWS, Mode MODE, Order ORDER>
+__device__ __forceinline__ bool find_shared(const CacheAttendParams& P, int pos, Part* out, int64_t* row, int* first) {
+  const int b = __builtin_amdgcn_readfirstlane((MODE == kOwn ? P.share.own_part : P.share.prefix_part)[pos]);
+  if (b < 0) return false;
+  const int4 x = MODE == kOwn ? P.share.own[3 * b] : P.share.prefix[2 * b];
+  const int4 y = MODE == kOwn ? P.share.own[3 * b + 2] : P.share.prefix[2 * b + 1];
+  out->b = b;
+  out->q = y.x;
+  out->kv = MODE == kOwn ? y.y : y.y * kBlock;
+  out->splits = x.y;
+  const int rows = y.x * P.s.G, tiles = (rows + ROWS - 1) / ROWS, all = (rows + 15) / 16 * 16;
+  locate<ORDER>(P, pos - x.x, tiles, 0, out);
+  *row = (int64_t)x.z + (int64_t)out->splits * (out->kvh * all + out->tile * ROWS) + out->split * min(ROWS, all - out->tile * ROWS);
+  if (MODE == kOwn && x.z < 0) *row = -1;
+  *first = MODE == kOwn ? x.w : 0;
+  out->slot = x.w;                          // kPrefix: the group's first entry in `row`
+  return true;
+}
+
+// Row r of a part: its request and token, as request * rows + token, and the last key it sees; x < 0: no row.
+template <Mode MODE>
+__device__ __forceinline__ int2 row_of(const CacheAttendParams& P, const Part& u, int r) {
+  if (r >= u.q * P.s.G) return make_int2(-1, -1);
+  const int i = r / P.s.G;
+  if (MODE == kPrefix) return P.share.row[u.slot + i];
+  return make_int2(u.b * P.s.rows + i, u.kv - u.q + i);
 }
 
 // Pages that the rows of a tile see (the last row sees most).
@@ -411,13 +463,13 @@ __device__ __forceinline__ void store_row(const CacheAttendParams& P, const Part
       make_uint2(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv));
 }
 
-// The waves' sums of a part: O, or the part's slot.  seen: a key of the row has been
+// The waves' sums of a part: O, or (row >= 0) rows `row` .. of the workspace.  seen: a key of the row has been
 // looked at.  Each wave brings its own to the rows' maxima first (and, where the part is
 // the whole, divides by the sums), so what is left are plain sums, 16 rows at a time, of
 // values that lie in LDS as the lanes hold them.  s_o: NW D 16 floats, 16-byte aligned, may be
 // what the waves still use on entry; s_ml: [NW][16 RT], may not.
 template <int D, int RT, int NW>
-__device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Part& u, float* s_o, float2* s_ml,
+__device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Part& u, int64_t row, float* s_o, float2* s_ml,
                                             f32x4 (&acc)[RT][D / 16], const float (&m_run)[RT], const float (&l_run)[RT],
                                             const bool (&seen)[RT]) {
   constexpr int ROWS = 16 * RT, DT = D / 16;
@@ -429,7 +481,6 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
     if (g == 0) s_ml[w * ROWS + 16 * rt + c16] = make_float2(seen[rt] ? m_run[rt] : -__builtin_huge_valf(), l);
   }
   __syncthreads();
-  const size_t slot = (size_t)u.slot + u.split;
   f32x4* const so = reinterpret_cast<f32x4*>(s_o);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -447,8 +498,8 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
       l += a * ml[v].y;
       if (v == w) mine = a;
     }
-    if (u.splits == 1) mine *= reciprocal(M, l);
-    else if (w == 0 && g == 0) P.part_ml[slot * ROWS + rr] = make_float2(M, l);
+    if (row < 0) mine *= reciprocal(M, l);
+    else if (w == 0 && g == 0 && u.tile * ROWS + rr < u.q * s.G) P.part_ml[row + rr] = make_float2(M, l);
     if (rt > 0) __syncthreads();
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
@@ -465,8 +516,8 @@ __device__ __forceinline__ void finish_part(const CacheAttendParams& P, const Pa
         f32x4 o = so[dt * 64 + lane];
 #pragma unroll
         for (int v = 1; v < NW; ++v) o += so[(v * DT + dt) * 64 + lane];
-        if (u.splits == 1) store_row(P, u, D, at_row, c, o, 1.0f);
-        else *reinterpret_cast<f32x4*>(P.part_o + (slot * ROWS + rr) * D + c) = o;
+        if (row < 0) store_row(P, u, D, at_row, c, o, 1.0f);
+        else *reinterpret_cast<f32x4*>(P.part_o + (row + rr) * D + c) = o;
       }
     }
   }
@@ -613,6 +664,14 @@ __global__ void __launch_bounds__(256) cache_join_rows_kernel(CacheAttendParams 
   }
   store_row(P, u, D, at_row, 4 * c, o, reciprocal(M, l));
 }
+
+inline size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+inline bool may_split(const CacheShape& s) { return s.max_pages > min_pages(s.d); }
+
+// Rows of a tile: as many as the call can have.
+inline int tile_rows(int d, int64_t rows) { return rows <= 16 ? 16 : rows <= 32 ? 32 : tile_rows_many(d); }
+inline int tile_rows(const CacheShape& s) { return tile_rows(s.d, (int64_t)s.rows * s.G); }
 
 inline int64_t tiles_bound(const CacheShape& s, int rows_of_a_tile) {
   return (int64_t)s.B * s.Hkv * (((int64_t)s.rows * s.G + rows_of_a_tile - 1) / rows_of_a_tile);

@@ -35,7 +35,7 @@ namespace {
 // rest.  Bound by HBM: 32 ragged requests of up to 8K (32/8 heads, d 128, 276 MB)
 // 53 us with the join, 5.2 TB/s (large copies reach 4.7 to 6.1); one of 128K (28/4 heads,
 // 134 MB) 30.3 us, of which the join 4.6.
-template <int D, int DT, int RT, int NW>
+template <int D, int DT, int RT, int NW, Mode MODE>
 __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendParams P) {
   constexpr int L = D / 32;                 // 16-byte loads of a lane: keys, and again values
   constexpr int ROWS = 16 * RT;
@@ -45,13 +45,20 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   Part u;
-  if (!find_part<ROWS, kParts>(P, blockIdx.x, &u)) return;
+  int64_t row = -1;
+  int first = 0;
+  if constexpr (MODE == kWhole) {
+    if (!find_part<ROWS, kParts>(P, blockIdx.x, &u)) return;
+    if (u.splits > 1) row = ((int64_t)u.slot + u.split) * ROWS;
+  } else {
+    if (!find_shared<ROWS, MODE, kParts>(P, blockIdx.x, &u, &row, &first)) return;
+  }
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.kvh = __builtin_amdgcn_readfirstlane(u.kvh);
   u.kv = __builtin_amdgcn_readfirstlane(u.kv);
-  const int n = pages_seen<ROWS>(P, u);
-  const int p0 = __builtin_amdgcn_readfirstlane(n * u.split / u.splits);
-  const int p1 = __builtin_amdgcn_readfirstlane(n * (u.split + 1) / u.splits);
+  const int n = MODE == kPrefix ? u.kv / kBlock : max(pages_seen<ROWS>(P, u) - first, 0);
+  const int p0 = __builtin_amdgcn_readfirstlane(first + n * u.split / u.splits);
+  const int p1 = __builtin_amdgcn_readfirstlane(first + n * (u.split + 1) / u.splits);
 
   // waves 2 j and 2 j + 1 take the halves of pages p0 + j, p0 + j + NW / 2, ...
   const int half = w & 1;
@@ -64,9 +71,16 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   for (int rt = 0; rt < RT; ++rt) {
     const int r = u.tile * ROWS + 16 * rt + c16;
     const bool ok = r < u.q * s.G;
-    const int i = ok ? r / s.G : 0, h = u.kvh * s.G + (ok ? r % s.G : 0);
+    int b = u.b, i = ok ? r / s.G : 0;
+    const int h = u.kvh * s.G + (ok ? r % s.G : 0);
     last[rt] = ok ? u.kv - u.q + i : -1;
-    const uint16_t* const q = P.Q + (((size_t)u.b * s.H + h) * s.rows + i) * D + 16 * g;
+    if constexpr (MODE == kPrefix) {
+      const int2 at = row_of<MODE>(P, u, r);
+      last[rt] = at.y;
+      b = max(at.x, 0) / s.rows;
+      i = max(at.x, 0) % s.rows;
+    }
+    const uint16_t* const q = P.Q + (((size_t)b * s.H + h) * s.rows + i) * D + 16 * g;
 #pragma unroll
     for (int x = 0; x < D / 64; ++x)
 #pragma unroll
@@ -77,7 +91,16 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
       }
   }
   // every valid row sees the keys up to here
-  const int all_see = u.kv - u.q + u.tile * ROWS / s.G;
+  int all_see = u.kv - u.q + u.tile * ROWS / s.G;
+  if constexpr (MODE == kPrefix) {
+    all_see = INT32_MAX;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+      if (u.tile * ROWS + 16 * rt + c16 < u.q * s.G) all_see = min(all_see, last[rt]);
+#pragma unroll
+    for (int o = 1; o < 16; o *= 2) all_see = min(all_see, __shfl_xor(all_see, o));
+    all_see = __builtin_amdgcn_readfirstlane(all_see);
+  }
 
   uint4 kx[L], vx[L];
   auto bytes_of = [&](int page) {
@@ -195,25 +218,30 @@ __global__ void __launch_bounds__(64 * NW) cache_attend_rows_kernel(CacheAttendP
   bool seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = key_first <= last[rt];
-  finish_part<D, RT, NW>(P, u, s_o, &s_ml[0][0], acc, m_run, l_run, seen);
+  finish_part<D, RT, NW>(P, u, row, s_o, &s_ml[0][0], acc, m_run, l_run, seen);
 }
-
-bool may_split(const CacheShape& s) { return s.max_pages > min_pages(s.d); }
 
 template <int D, int DT, int RT>
 hipError_t attend_rows(const CacheAttendParams& P, hipStream_t stream) {
   constexpr int NW = 4, ROWS = 16 * RT;
   const int64_t units = tiles_bound(P.s, ROWS);
   launch_schedule<ROWS>(P, stream);
-  cache_attend_rows_kernel<D, DT, RT, NW><<<(unsigned)(units + (P.splits ? kTarget : 0)), 64 * NW, 0, stream>>>(P);
+  cache_attend_rows_kernel<D, DT, RT, NW, kWhole><<<(unsigned)(units + (P.splits ? kTarget : 0)), 64 * NW, 0, stream>>>(P);
   if (P.splits) launch_join<D, ROWS>(P, stream);
   return hipGetLastError();
 }
 
-// Rows of a tile: as many as the call can have.
-int tile_rows(const CacheShape& s) {
-  const int64_t rows = (int64_t)s.rows * s.G;
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : tile_rows_many(s.d);
+template <int D, int DT, int RT>
+void shared_rows(const CacheAttendParams& P, Mode mode, unsigned parts, hipStream_t stream) {
+  if (mode == kOwn) cache_attend_rows_kernel<D, DT, RT, 4, kOwn><<<parts, 256, 0, stream>>>(P);
+  else cache_attend_rows_kernel<D, DT, RT, 4, kPrefix><<<parts, 256, 0, stream>>>(P);
+}
+
+template <int D, int DT>
+void shared_rows(const CacheAttendParams& P, Mode mode, unsigned parts, int rows, hipStream_t stream) {
+  if constexpr (D != 256)
+    if (rows == 32) return shared_rows<D, DT, 2>(P, mode, parts, stream);
+  shared_rows<D, DT, 1>(P, mode, parts, stream);
 }
 
 // At d 256 32 rows leave one wave per SIMD here, two in cache_tiles.hip (8 requests of
@@ -229,8 +257,14 @@ hipError_t attend(const CacheAttendParams& P, hipStream_t stream) {
 
 }  // namespace
 
+void launch_shared_rows(const CacheAttendParams& P, Mode mode, unsigned parts, int rows, hipStream_t stream) {
+  const bool f8 = P.s.dtype == UGBS_E4M3;
+  if (P.s.d == 64) (f8 ? shared_rows<64, UGBS_E4M3> : shared_rows<64, UGBS_INT8>)(P, mode, parts, rows, stream);
+  else if (P.s.d == 128) (f8 ? shared_rows<128, UGBS_E4M3> : shared_rows<128, UGBS_INT8>)(P, mode, parts, rows, stream);
+  else (f8 ? shared_rows<256, UGBS_E4M3> : shared_rows<256, UGBS_INT8>)(P, mode, parts, rows, stream);
+}
+
 // Workspace: the parts' sums, their (maximum, sum) pairs, and a large batch's schedule.
-static size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 static size_t schedule_at(const CacheShape& s) {
   return may_split(s) ? (size_t)kSlots * tile_rows(s) * (s.d * sizeof(float) + sizeof(float2)) : 0;
 }
@@ -246,7 +280,7 @@ size_t cache_attend_workspace(const CacheShape& s) {
 hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uint8_t* cache, const float* scales,
                                const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, uint16_t* O,
                                void* workspace, hipStream_t stream) {
-  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, min_pages(s.d)};
+  CacheAttendParams P{s, Q, cache, scales, table, kv_lens, q_lens, O, nullptr, nullptr, 0.f, false, {}, min_pages(s.d), {}};
   P.scale_log2 = s.scale * 1.4426950408889634f;
   P.splits = may_split(s);
   if (P.splits) {

@@ -34,6 +34,13 @@ hipError_t launch_cache_attend(const CacheShape& s, const uint16_t* Q, const uin
                                const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, uint16_t* O,
                                void* workspace, hipStream_t stream);
 size_t cache_attend_workspace(const CacheShape& s);
+hipError_t launch_cache_share(const CacheShape& s, const int32_t* group, const int32_t* table, const int32_t* kv_lens,
+                              const int32_t* q_lens, void* share, hipStream_t stream);
+hipError_t launch_cache_attend_shared(const CacheShape& s, const uint16_t* Q, const uint8_t* cache, const float* scales,
+                                      const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens, const void* share,
+                                      uint16_t* O, void* workspace, hipStream_t stream);
+size_t cache_share_bytes(const CacheShape& s);
+size_t cache_shared_workspace(const CacheShape& s);
 
 namespace {
 

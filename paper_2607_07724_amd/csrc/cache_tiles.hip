@@ -98,7 +98,7 @@ __device__ __forceinline__ uint32_t split_row(uint4* v) {
 }
 
 // One part: RT tiles of 16 rows against pages p0 .. p1 - 1.
-template <int D, int DT, int RT, int QR, int NW, int WPE, bool ONCE>
+template <int D, int DT, int RT, int QR, int NW, int WPE, bool ONCE, Mode MODE>
 __global__ void __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPE, WPE)))
 cache_tiles_kernel(CacheAttendParams P) {
   constexpr int L = D / 32, E = D / 64;     // loads of a half page's keys (values); 64-channel steps
@@ -113,16 +113,24 @@ cache_tiles_kernel(CacheAttendParams P) {
   const CacheShape& s = P.s;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, c16 = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  __shared__ int s_last[MODE == kPrefix ? ROWS : 1];        // the last key that a row sees, -1: no row
   Part u;
-  if (!find_part<ROWS, kGroups>(P, blockIdx.x, &u)) return;
+  int64_t row = -1;
+  int first = 0;
+  if constexpr (MODE == kWhole) {
+    if (!find_part<ROWS, kGroups>(P, blockIdx.x, &u)) return;
+    if (u.splits > 1) row = ((int64_t)u.slot + u.split) * ROWS;
+  } else {
+    if (!find_shared<ROWS, MODE, kGroups>(P, blockIdx.x, &u, &row, &first)) return;
+  }
   u.b = __builtin_amdgcn_readfirstlane(u.b);
   u.kvh = __builtin_amdgcn_readfirstlane(u.kvh);
   u.kv = __builtin_amdgcn_readfirstlane(u.kv);
   u.q = __builtin_amdgcn_readfirstlane(u.q);
   u.tile = __builtin_amdgcn_readfirstlane(u.tile);
-  const int n = pages_seen<ROWS>(P, u);
-  const int p0 = __builtin_amdgcn_readfirstlane(n * u.split / u.splits);
-  const int p1 = __builtin_amdgcn_readfirstlane(n * (u.split + 1) / u.splits);
+  const int n = MODE == kPrefix ? u.kv / kBlock : max(pages_seen<ROWS>(P, u) - first, 0);
+  const int p0 = __builtin_amdgcn_readfirstlane(first + n * u.split / u.splits);
+  const int p1 = __builtin_amdgcn_readfirstlane(first + n * (u.split + 1) / u.splits);
 
   const int half = w & 1;
   const uint8_t* const cache = P.cache + (size_t)u.kvh * 2 * (kBlock * D) + half * kTile;
@@ -159,9 +167,16 @@ cache_tiles_kernel(CacheAttendParams P) {
   for (int rt = 0; rt < RT; ++rt) {
     const int r = u.tile * ROWS + 16 * rt + c16;
     const bool ok = r < u.q * s.G;
-    const int i = ok ? r / s.G : 0, h = u.kvh * s.G + (ok ? r % s.G : 0);
+    int b = u.b, i = ok ? r / s.G : 0;
+    const int h = u.kvh * s.G + (ok ? r % s.G : 0);
+    if constexpr (MODE == kPrefix) {
+      const int2 at = row_of<MODE>(P, u, r);
+      b = max(at.x, 0) / s.rows;
+      i = max(at.x, 0) % s.rows;
+      if (w == 0 && g == 0) s_last[16 * rt + c16] = at.y;
+    }
     if (F8 ? w == rt : rt < QR || w == rt % NW) {
-      const uint16_t* const q = P.Q + (((size_t)u.b * s.H + h) * s.rows + i) * D + 16 * g;
+      const uint16_t* const q = P.Q + (((size_t)b * s.H + h) * s.rows + i) * D + 16 * g;
       uint4 v[2 * E];
 #pragma unroll
       for (int x = 0; x < 2 * E; ++x) {
@@ -181,7 +196,7 @@ cache_tiles_kernel(CacheAttendParams P) {
       }
     }
   }
-  if constexpr (QR < RT || F8) __syncthreads();
+  if constexpr (QR < RT || F8 || MODE == kPrefix) __syncthreads();
   if constexpr (F8) {
     static_assert(RT <= NW && 2 * E * 1024 <= kTile, "a row tile to a wave, in the place of its values");
 #pragma unroll
@@ -200,9 +215,16 @@ cache_tiles_kernel(CacheAttendParams P) {
   // the last key that the lane's row in tile rt sees (asked for at the ends of requests only)
   auto last = [&](int rt) {
     const int r = u.tile * ROWS + 16 * rt + (int)here(c16);
+    if constexpr (MODE == kPrefix) return s_last[16 * rt + (int)here(c16)];
     return r < u.q * s.G ? u.kv - u.q + r / s.G : -1;
   };
-  const int all_see = u.kv - u.q + u.tile * ROWS / s.G;   // every valid row sees the keys up to here
+  int all_see = u.kv - u.q + u.tile * ROWS / s.G;         // every valid row sees the keys up to here
+  if constexpr (MODE == kPrefix) {
+    all_see = lane < min(ROWS, u.q * s.G - u.tile * ROWS) ? s_last[lane] : INT32_MAX;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) all_see = min(all_see, __shfl_xor(all_see, o));
+    all_see = __builtin_amdgcn_readfirstlane(all_see);
+  }
 
   f32x4 acc[RT][D / 16];
   float m_run[RT], l_run[RT];
@@ -386,7 +408,7 @@ cache_tiles_kernel(CacheAttendParams P) {
   bool seen[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) seen[rt] = key_first <= last(rt);
-  finish_part<D, RT, NW>(P, u, reinterpret_cast<float*>(s_mem), s_ml, acc, m_run, l_run, seen);
+  finish_part<D, RT, NW>(P, u, row, reinterpret_cast<float*>(s_mem), s_ml, acc, m_run, l_run, seen);
 }
 
 template <int D, int DT, int RT, int QR, int WPE>
@@ -396,13 +418,36 @@ hipError_t tiles(const CacheAttendParams& P, hipStream_t stream) {
   const int64_t units = tiles_bound(P.s, ROWS);
   launch_schedule<ROWS>(P, stream);
   const unsigned grid = (unsigned)(units + (P.splits ? kTarget : 0));
-  if ((int64_t)P.s.rows * P.s.G <= ROWS) cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true><<<grid, 64 * NW, 0, stream>>>(P);
-  else cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false><<<grid, 64 * NW, 0, stream>>>(P);
+  if ((int64_t)P.s.rows * P.s.G <= ROWS) cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true, kWhole><<<grid, 64 * NW, 0, stream>>>(P);
+  else cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false, kWhole><<<grid, 64 * NW, 0, stream>>>(P);
   if (P.splits) launch_join<D, ROWS>(P, stream);
   return hipGetLastError();
 }
 
+template <int D, int DT, int RT, int QR, int WPE>
+void shared_tiles(const CacheAttendParams& P, Mode mode, unsigned parts, bool once, hipStream_t stream) {
+  constexpr int NW = 4;
+  if (mode == kPrefix) {
+    if (once) cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true, kPrefix><<<parts, 64 * NW, 0, stream>>>(P);
+    else cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false, kPrefix><<<parts, 64 * NW, 0, stream>>>(P);
+    return;
+  }
+  if constexpr (D == 256)                  // 33 to 64 rows of a request are two tiles
+    if (!once) {
+      cache_tiles_kernel<D, DT, RT, QR, NW, WPE, false, kOwn><<<parts, 64 * NW, 0, stream>>>(P);
+      return;
+    }
+  cache_tiles_kernel<D, DT, RT, QR, NW, WPE, true, kOwn><<<parts, 64 * NW, 0, stream>>>(P);
+}
+
 }  // namespace
+
+void launch_shared_tiles(const CacheAttendParams& P, Mode mode, unsigned parts, bool once, hipStream_t stream) {
+  const bool f8 = P.s.dtype == UGBS_E4M3;
+  if (P.s.d == 64) (f8 ? shared_tiles<64, UGBS_E4M3, 4, 4, 3> : shared_tiles<64, UGBS_INT8, 4, 4, 3>)(P, mode, parts, once, stream);
+  else if (P.s.d == 128) (f8 ? shared_tiles<128, UGBS_E4M3, 4, 2, 2> : shared_tiles<128, UGBS_INT8, 4, 2, 2>)(P, mode, parts, once, stream);
+  else (f8 ? shared_tiles<256, UGBS_E4M3, 2, 2, 2> : shared_tiles<256, UGBS_INT8, 2, 2, 2>)(P, mode, parts, once, stream);
+}
 
 hipError_t launch_cache_tiles(const CacheAttendParams& P, hipStream_t stream) {
   const bool f8 = P.s.dtype == UGBS_E4M3;
