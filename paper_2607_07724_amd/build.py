@@ -51,7 +51,8 @@ CFLAGS = [
 EXTRA_FLAGS = {"score_select.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "attend_keys.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
                "cache_attend.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "cache_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "cache_tiles.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "cache_share.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 PACKED_FP32 = re.compile(r"\bv_pk_(add|mul|fma)_f32\b")
 

@@ -33,15 +33,15 @@ struct Schedule {
 // head h of rows R in all (R a multiple of 16) begins at row
 //   before + splits (h R + t ROWS) + split min(ROWS, R - t ROWS).
 struct Share {
-  int4* own;          // [B][3]: (parts before, parts of a tile, rows before or -1: written to O, the first page that is its own),
-                      //   (rows before of its group's prefix or -1, parts of a tile there, first new token in the group, group's R),
-                      //   (new tokens, cached tokens, -, -)
-  int4* prefix;       // [B][2], of leaders: (parts before, parts of a tile, rows before, first entry in `row`), (new tokens, pages, -, -)
-  int32_t* own_part;  // [own_parts]: the request, -1 behind the last part
-  int32_t* prefix_part;   // [prefix_parts]: the leader, -1 behind the last part
-  int2* row;          // [B rows]: new tokens of the groups: request * rows + token, the last key it sees
+  int4* own;          // [B][2]: (new tokens, parts of a tile, rows before or -1: written to O, common pages),
+                      //   (rows before of its group's prefix or -1, parts of a tile there, first new token in the group, group's R)
+  int4* prefix;       // [B][2], of leaders: (new tokens, parts of a tile, rows before, pages), (first entry in `row`; its own cached tokens, -, -)
+  int4* part;         // [parts][2]: (request or leader, -1: none; kv head, of a prefix + kOfPrefix; tile; first page),
+                      //   (behind its last page; row of its sums or -1; new tokens; cached tokens or, of a prefix, first entry in `row`)
+  int2* row;          // [B rows G]: rows of the groups: where its query of the first kv head lies (a row of Q), the last key it sees
   int4* found;        // [B]: leader (-1: alone), pages in common with it, new tokens of the group's requests before
 };
+constexpr int kOfPrefix = 1 << 24;
 
 struct CacheAttendParams {
   CacheShape s;
@@ -67,9 +67,6 @@ enum Mode { kWhole, kOwn, kPrefix };
 
 // Tiles of 64 (d 256: 32) rows, where rows are many (cache_tiles.hip).
 hipError_t launch_cache_tiles(const CacheAttendParams& P, hipStream_t stream);
-void launch_shared_tiles(const CacheAttendParams& P, Mode mode, unsigned parts, bool once, hipStream_t stream);
-// Tiles of 16 or 32 rows (cache_attend.hip).
-void launch_shared_rows(const CacheAttendParams& P, Mode mode, unsigned parts, int rows_of_a_tile, hipStream_t stream);
 constexpr int tile_rows_many(int d) { return d == 256 ? 32 : 64; }
 
 namespace {
@@ -339,33 +336,11 @@ __global__ void __launch_bounds__(kScheduleThreads) cache_schedule_kernel(CacheA
   if (blockIdx.x == 0 && tid < kTarget) P.schedule.join[tid] = tid < total[2] ? request_at(s_joins, tid) : -1;
 }
 
-// A part of a shared batch; *row: where its sums go, -1: it is its rows' only one.  *first: its first page.
-template <int ROWS, Mode MODE, Order ORDER>
-__device__ __forceinline__ bool find_shared(const CacheAttendParams& P, int pos, Part* out, int64_t* row, int* first) {
-  const int b = __builtin_amdgcn_readfirstlane((MODE == kOwn ? P.share.own_part : P.share.prefix_part)[pos]);
-  if (b < 0) return false;
-  const int4 x = MODE == kOwn ? P.share.own[3 * b] : P.share.prefix[2 * b];
-  const int4 y = MODE == kOwn ? P.share.own[3 * b + 2] : P.share.prefix[2 * b + 1];
-  out->b = b;
-  out->q = y.x;
-  out->kv = MODE == kOwn ? y.y : y.y * kBlock;
-  out->splits = x.y;
-  const int rows = y.x * P.s.G, tiles = (rows + ROWS - 1) / ROWS, all = (rows + 15) / 16 * 16;
-  locate<ORDER>(P, pos - x.x, tiles, 0, out);
-  *row = (int64_t)x.z + (int64_t)out->splits * (out->kvh * all + out->tile * ROWS) + out->split * min(ROWS, all - out->tile * ROWS);
-  if (MODE == kOwn && x.z < 0) *row = -1;
-  *first = MODE == kOwn ? x.w : 0;
-  out->slot = x.w;                          // kPrefix: the group's first entry in `row`
-  return true;
-}
-
-// Row r of a part: its request and token, as request * rows + token, and the last key it sees; x < 0: no row.
-template <Mode MODE>
+// Row r of a part of a prefix: its row of Q, the last key it sees; (0, -1): there is none.
 __device__ __forceinline__ int2 row_of(const CacheAttendParams& P, const Part& u, int r) {
-  if (r >= u.q * P.s.G) return make_int2(-1, -1);
-  const int i = r / P.s.G;
-  if (MODE == kPrefix) return P.share.row[u.slot + i];
-  return make_int2(u.b * P.s.rows + i, u.kv - u.q + i);
+  if (r >= u.q * P.s.G) return make_int2(0, -1);
+  const int2 at = P.share.row[(size_t)u.slot * P.s.G + r];
+  return make_int2(at.x + u.kvh * P.s.G * P.s.rows, at.y);
 }
 
 // Pages that the rows of a tile see (the last row sees most).

@@ -10,7 +10,10 @@
 // ugbs_cache_share finds, once a step, what the requests of a group have in common (their table
 // rows are compared, so nothing but the table says what is shared) and lays the parts out,
 // as ugbs_cache_attend does for itself; the launches of a layer only look their part up.
-#include "cache_attend.h"
+#include <algorithm>
+
+#include "cache_rows.h"
+#include "cache_tiles.h"
 
 namespace ugbs {
 namespace {
@@ -27,19 +30,26 @@ bool shares(const CacheShape& s) {
 
 struct Sizes {
   int own_rows, prefix_rows;          // of a tile
-  int64_t own_parts, prefix_parts;    // at most
+  int64_t parts;                      // at most
   int64_t sum_rows;                   // rows of the parts' sums, at most
 };
 
-// A part more than the tiles for each of kTarget at most; a group has two requests at least.
+// Tiles of 32 rows are not worth kernels of their own for prefixes (4 requests of 7 rows each behind 128K: the
+// tile of 64 is bound by the same bytes).
+int prefix_tile_rows(int d, int64_t rows) { return rows <= 16 ? 16 : tile_rows_many(d); }
+
+// Workgroups that the chip holds at once (two a CU, three with the small tiles of d 64).
+int places_of(int d, int prefix_rows) { return d == 64 && prefix_rows != 16 ? kTarget / 2 * 3 : kTarget; }
+
+// More parts than tiles: by `places` at most; a group has two requests at least.
 Sizes sizes_of(const CacheShape& s) {
   const int64_t all = (int64_t)s.B * s.rows * s.G, groups = s.B / 2;
   Sizes z;
   z.own_rows = tile_rows(s);
-  z.prefix_rows = tile_rows(s.d, all);
-  z.own_parts = tiles_bound(s, z.own_rows) + kTarget;
-  z.prefix_parts = s.Hkv * (all / z.prefix_rows + groups) + kTarget;
-  z.sum_rows = s.Hkv * (s.B * (((int64_t)s.rows * s.G + 15) / 16 * 16) + all + 15 * groups) + kTarget * (z.own_rows + z.prefix_rows);
+  z.prefix_rows = prefix_tile_rows(s.d, all);
+  const int more = places_of(s.d, z.prefix_rows);
+  z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + more + 8;
+  z.sum_rows = s.Hkv * (s.B * (((int64_t)s.rows * s.G + 15) / 16 * 16) + all + 15 * groups) + more * std::max(z.own_rows, z.prefix_rows);
   return z;
 }
 
@@ -53,11 +63,10 @@ size_t lay_out(const CacheShape& s, void* at, Share* share) {
     n += align256(bytes);
     return p;
   };
-  share->own = reinterpret_cast<int4*>(take(3 * sizeof(int4) * s.B));
+  share->own = reinterpret_cast<int4*>(take(2 * sizeof(int4) * s.B));
   share->prefix = reinterpret_cast<int4*>(take(2 * sizeof(int4) * s.B));
-  share->own_part = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * z.own_parts));
-  share->prefix_part = reinterpret_cast<int32_t*>(take(sizeof(int32_t) * z.prefix_parts));
-  share->row = reinterpret_cast<int2*>(take(sizeof(int2) * s.B * s.rows));
+  share->part = reinterpret_cast<int4*>(take(2 * sizeof(int4) * z.parts));
+  share->row = reinterpret_cast<int2*>(take(sizeof(int2) * s.B * s.rows * s.G));
   share->found = reinterpret_cast<int4*>(take(sizeof(int4) * s.B));
   return n;
 }
@@ -114,57 +123,75 @@ __global__ void __launch_bounds__(256) share_compare_kernel(CacheAttendParams P,
   }
 }
 
-// Sums over the workgroup, before this thread and in all.
-constexpr int kPlanThreads = 1024, kPer = UGBS_MAX_REQUESTS / kPlanThreads;
-__device__ __forceinline__ float sum_all(float x, float* s_wave) {
-  x = sum_wave(x);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) s_wave[threadIdx.x >> 6] = x;
-  __syncthreads();
-  x = 0.f;
+// Sums over the workgroup of N numbers of each thread: in all, and before it.
+template <int NW, int N>
+__device__ __forceinline__ void sum_all(float (&x)[N], float (*s_wave)[NW]) {
 #pragma unroll
-  for (int v = 0; v < kPlanThreads / 64; ++v) x += s_wave[v];
-  return x;
-}
-__device__ __forceinline__ int sum_before(int x, int* s_wave, int* total) {
-  const int upto = scan_add(x), w = threadIdx.x >> 6;
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63) s_wave[w] = upto;
-  __syncthreads();
-  int before = upto - x;
-  *total = 0;
-#pragma unroll
-  for (int v = 0; v < kPlanThreads / 64; ++v) {
-    if (v < w) before += s_wave[v];
-    *total += s_wave[v];
+  for (int y = 0; y < N; ++y) {
+    x[y] = sum_wave(x[y]);
+    if ((threadIdx.x & 63) == 0) s_wave[y][threadIdx.x >> 6] = x[y];
   }
-  return before;
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < N; ++y) {
+    x[y] = 0.f;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) x[y] += s_wave[y][v];
+  }
+}
+template <int NW, int N>
+__device__ __forceinline__ void sum_before(const int (&x)[N], int (&before)[N], int (&total)[N], int (*s_wave)[NW]) {
+  const int w = threadIdx.x >> 6;
+#pragma unroll
+  for (int y = 0; y < N; ++y) {
+    before[y] = scan_add(x[y]);
+    if ((threadIdx.x & 63) == 63) s_wave[y][w] = before[y];
+    before[y] -= x[y];
+    total[y] = 0;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int y = 0; y < N; ++y)
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      if (v < w) before[y] += s_wave[y][v];
+      total[y] += s_wave[y][v];
+    }
 }
 
-// The parts.  Every workgroup forms the sums over all requests (4 a thread); the first one writes
-// the requests' entries, all write their share of the lists.
-__global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendParams P, int own_rows, int prefix_rows, int own_parts,
-                                                                  int prefix_parts) {
-  __shared__ int s_a[UGBS_MAX_REQUESTS], s_b[UGBS_MAX_REQUESTS], s_c[UGBS_MAX_REQUESTS];
-  __shared__ float s_sum[kPlanThreads / 64];
-  __shared__ int s_scan[kPlanThreads / 64];
+// What a part costs, in pages of a prefix part: its start and end; a page and the start of a part of own pages.
+constexpr float kStart = 8.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
+constexpr int kTimes = 6;                 // candidates for the longest part's time, each
+constexpr float kLonger = 0.15f;          // so much longer than the one before
+
+// The parts: the work of one workgroup, PER requests a thread.
+template <int THREADS, int PER>
+__global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P, int own_rows, int prefix_rows, int parts, float places) {
+  constexpr int NW = THREADS / 64, MOST = THREADS * PER;
+  __shared__ int s_a[MOST], s_b[MOST], s_c[MOST];
+  __shared__ float s_sum[4][NW], s_parts[kTimes][NW];
+  __shared__ int s_scan[5][NW];
   const int tid = threadIdx.x, B = P.s.B, G = P.s.G, Hkv = P.s.Hkv, most = P.s.max_pages * kBlock;
-  for (int b = tid; b < B; b += kPlanThreads) {
+  for (int b = tid; b < B; b += THREADS) {
     s_a[b] = INT32_MAX;
     s_b[b] = s_c[b] = 0;
   }
-  __syncthreads();
-  int4 found[kPer];
-  Lengths own[kPer], pre[kPer];
+  int4 found[PER];
+  Lengths own[PER], pre[PER];
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int b = kPer * tid + k;
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k;
     found[k] = make_int4(-1, 0, 0, 0);
     own[k] = pre[k] = Lengths{0, 0, 0, 0};
-    if (b >= B) continue;
-    found[k] = P.share.found[b];
-    own[k].q = min(max(P.q_lens[b], 0), P.s.rows);
-    own[k].kv = min(max(P.kv_lens[b], 0), most);
+    if (b < B) {
+      found[k] = P.share.found[b];
+      own[k].q = min(max(P.q_lens[b], 0), P.s.rows);
+      own[k].kv = min(max(P.kv_lens[b], 0), most);
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
     const int l = found[k].x;
     if (l >= 0) {
       atomicMin(&s_a[l], found[k].y);                          // pages in common
@@ -173,10 +200,10 @@ __global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendPar
     }
   }
   __syncthreads();
-  int together[kPer];                                          // new tokens of the group, 0: nothing is shared
+  int together[PER];                                           // new tokens of the group
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int b = kPer * tid + k, l = found[k].x;
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k, l = found[k].x;
     together[k] = 0;
     int pages = 0;
     if (l >= 0 && s_a[l] * (s_c[l] - 1) >= kLeastSaved) {
@@ -192,21 +219,58 @@ __global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendPar
       pre[k].pages = pages;
     }
   }
-  auto per_part = [&](const Lengths (&r)[kPer], int rows) {
-    float work = 0.f, tiles = 0.f, wide = 0.f;
+  // Pages a part, from the time that the longest may take: all parts together, spread evenly over the chip's
+  // places, and longer until there is a place for each (where there are more tiles than places: as it is).
+  float sums[4] = {0.f, 0.f, 0.f, 0.f};                        // work and tiles, own and of prefixes
 #pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      work = __builtin_fmaf((float)r[k].tiles, (float)r[k].pages, work);
-      tiles += (float)r[k].tiles;
-    }
-    work = sum_all(work, s_sum);
-    tiles = sum_all(tiles, s_sum);
+  for (int k = 0; k < PER; ++k) {
+    sums[0] = __builtin_fmaf((float)own[k].tiles, (float)own[k].pages, sums[0]);
+    // (the last tile of a group may be one of few rows)
+    const float few = prefix_rows > 32 && pre[k].q * G - (pre[k].tiles - 1) * prefix_rows <= 32 ? 1.0f - kOwnPage : 0.0f;
+    sums[1] = __builtin_fmaf((float)pre[k].tiles - few, (float)pre[k].pages, sums[1]);
+    sums[2] += (float)own[k].tiles;
+    sums[3] += (float)pre[k].tiles;
+  }
+  sum_all<NW>(sums, s_sum);
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)
-      if (is_wide(P, r[k], work)) wide += (float)r[k].tiles;
-    return pages_per_part(P, rows, work, tiles, sum_all(wide, s_sum));
+  for (int y = 0; y < 4; ++y) sums[y] *= (float)Hkv;
+  const bool alike = own_rows == prefix_rows;
+  const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart, least = (float)P.min_pages, each = 1.0f / places;
+  auto pages_of_time = [&](float time, int* o, int* p) {
+    *o = *p = UGBS_MAX_BLOCKS;
+    if (!P.splits) return;
+    // (no more than `places` parts above the tiles, own and of prefixes together)
+    const float most = fmaxf((sums[0] + sums[1]) * each, least), x = fmaxf((time - start) / cost, most), y = fmaxf(time - kStart, most);
+    *o = x < (float)UGBS_MAX_BLOCKS ? (int)x + 1 : UGBS_MAX_BLOCKS;
+    *p = y < (float)UGBS_MAX_BLOCKS ? (int)y + 1 : UGBS_MAX_BLOCKS;
   };
-  const int per_own = per_part(own, own_rows), per_pre = per_part(pre, prefix_rows);
+  float time = 0.f, n_o = sums[2], n_p = sums[3];
+#pragma unroll
+  for (int y = 0; y < 4; ++y) {
+    time = (cost * sums[0] + sums[1] + start * n_o + kStart * n_p) * each;
+    n_o = fmaxf(sums[2], sums[0] * cost / fmaxf(time - start, 1.0f));
+    n_p = fmaxf(sums[3], sums[1] / fmaxf(time - kStart, 1.0f));
+  }
+  float longer = 1.0f;
+  if (sums[2] + sums[3] <= places) {
+    float parts_at[kTimes];
+#pragma unroll
+    for (int y = 0; y < kTimes; ++y) {
+      int o, p;
+      pages_of_time(time * (1.0f + kLonger * y), &o, &p);
+      const float io = 1.0f / o, ip = 1.0f / p;
+      parts_at[y] = 0.f;
+#pragma unroll
+      for (int k = 0; k < PER; ++k)
+        parts_at[y] += own[k].tiles * fmaxf(ceilf(own[k].pages * io), 1.0f) + pre[k].tiles * fmaxf(ceilf(pre[k].pages * ip), 1.0f);
+    }
+    sum_all<NW>(parts_at, s_parts);
+#pragma unroll
+    for (int y = kTimes - 1; y >= 0; --y)
+      if (parts_at[y] * (float)Hkv <= places) longer = 1.0f + kLonger * y;
+  }
+  int per_own, per_pre;
+  pages_of_time(time * longer, &per_own, &per_pre);
   // parts and rows of sums of the requests and of the groups, and the groups' new tokens
   int n[5] = {0, 0, 0, 0, 0}, at[5], total[5];
   auto count = [&](int k, int (&x)[5]) {
@@ -218,60 +282,47 @@ __global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendPar
     x[4] = pre[k].q;
   };
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
+  for (int k = 0; k < PER; ++k) {
     int x[5];
     count(k, x);
 #pragma unroll
     for (int y = 0; y < 5; ++y) n[y] += x[y];
   }
-#pragma unroll
-  for (int y = 0; y < 5; ++y) at[y] = sum_before(n[y], s_scan, &total[y]);
+  sum_before<NW>(n, at, total, s_scan);
   at[3] += total[1];                                           // behind the requests' own
-  // (the barriers of the sums are behind the last reads of s_a .. s_c)
-  int first[kPer][5];
+  // (the barriers of the sums are behind the last reads of s_a and s_b)
 #pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int b = kPer * tid + k;
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k, so = splits_of(own[k], per_own), sp = splits_of(pre[k], per_pre);
     int x[5];
     count(k, x);
-#pragma unroll
-    for (int y = 0; y < 5; ++y) {
-      first[k][y] = at[y];
-      at[y] += x[y];
-    }
-    if (b < B && pre[k].tiles > 0) {
-      s_a[b] = first[k][3];
-      s_b[b] = splits_of(pre[k], per_pre);
-      s_c[b] = first[k][4];
-    }
-  }
-  __syncthreads();
-  if (blockIdx.x == 0) {
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {
-      const int b = kPer * tid + k, l = found[k].x, so = splits_of(own[k], per_own), pages = found[k].y;
-      if (b >= B) continue;
-      int4* const o = P.share.own + 3 * b;
-      o[0] = make_int4(first[k][0], so, so > 1 || pages > 0 ? first[k][1] : -1, pages);
-      o[1] = pages > 0 ? make_int4(s_a[l], s_b[l], found[k].z, (together[k] * G + 15) / 16 * 16) : make_int4(-1, 0, 0, 0);
-      o[2] = make_int4(own[k].q, own[k].kv, 0, 0);
-      P.share.prefix[2 * b] = make_int4(first[k][2], splits_of(pre[k], per_pre), first[k][3], first[k][4]);
-      P.share.prefix[2 * b + 1] = make_int4(pre[k].q, pre[k].pages, 0, 0);
-      if (pages > 0)
-        for (int i = 0; i < own[k].q; ++i)
-          P.share.row[s_c[l] + found[k].z + i] = make_int2(b * P.s.rows + i, own[k].kv - own[k].q + i);
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int b = kPer * tid + k;
     if (b < B) {
-      s_a[b] = first[k][0];
-      s_b[b] = first[k][2];
+      s_a[b] = at[0];
+      s_b[b] = at[2];
+      P.share.own[2 * b] = make_int4(own[k].q, so, so > 1 || found[k].y > 0 ? at[1] : -1, found[k].y);
+      P.share.prefix[2 * b] = make_int4(pre[k].q, sp, at[3], pre[k].pages);
+      P.share.prefix[2 * b + 1] = make_int4(at[4], own[k].kv, 0, 0);
     }
+#pragma unroll
+    for (int y = 0; y < 5; ++y) at[y] += x[y];
   }
   __syncthreads();
+  // the requests' entries
+#pragma unroll
+  for (int k = 0; k < PER; ++k) {
+    const int b = PER * tid + k, l = found[k].x;
+    if (b >= B) continue;
+    int4 y = make_int4(-1, 0, 0, 0);
+    if (found[k].y > 0) {
+      const int4 of = P.share.prefix[2 * l];
+      const int map = P.share.prefix[2 * l + 1].x;
+      y = make_int4(of.z, of.y, found[k].z, (together[k] * G + 15) / 16 * 16);
+      int2* const row = P.share.row + (size_t)(map + found[k].z) * G;
+      for (int i = 0; i < own[k].q; ++i)
+        for (int g = 0; g < G; ++g) row[i * G + g] = make_int2((b * P.s.H + g) * P.s.rows + i, own[k].kv - own[k].q + i);
+    }
+    P.share.own[2 * b + 1] = y;
+  }
   // the last request with sums[b] <= i (those without parts have the same sum as the next)
   auto request_at = [&](const int* sums, int i) {
     int lo = 0, hi = B - 1;
@@ -282,10 +333,117 @@ __global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendPar
     }
     return lo;
   };
-  const int stride = gridDim.x * kPlanThreads;
-  for (int i = blockIdx.x * kPlanThreads + tid; i < own_parts; i += stride) P.share.own_part[i] = i < total[0] ? request_at(s_a, i) : -1;
-  for (int i = blockIdx.x * kPlanThreads + tid; i < prefix_parts; i += stride)
-    P.share.prefix_part[i] = i < total[2] ? request_at(s_b, i) : -1;
+  // The list: the parts of prefixes, which are longer, first.  (Spread among the others, so that each CU has
+  // one of each, 64 requests behind 8K tokens took 34.6 us for 32.9.)
+  const int behind = (total[2] + 7) / 8 * 8;
+  for (int i = tid; i < parts; i += THREADS) {
+    int4 x = make_int4(-1, 0, 0, 0), y = x;
+    if (i < behind + total[0]) {
+      const bool prefix = i < behind;
+      const int pos = prefix ? i : i - behind;
+      if (!prefix || pos < total[2]) {
+        const int b = request_at(prefix ? s_b : s_a, pos);
+        const int4 r = prefix ? P.share.prefix[2 * b] : P.share.own[2 * b], more = P.share.prefix[2 * b + 1];
+        const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size, all = (rows + 15) / 16 * 16;
+        Part u;
+        u.splits = r.y;
+        if (prefix) locate<kGroups>(P, pos - s_b[b], tiles, 0, &u);
+        else locate<kParts>(P, pos - s_a[b], tiles, 0, &u);
+        const int row = r.z < 0 ? -1 : r.z + u.splits * (u.kvh * all + u.tile * size) + u.split * min(size, all - u.tile * size);
+        int first = 0, pages = r.w;
+        if (!prefix) {
+          // pages that the tile's last row sees, behind the common ones
+          const int end = more.y - r.x + (min((u.tile + 1) * size, rows) - 1) / G + 1;
+          first = r.w;
+          pages = max((max(end, 0) + kBlock - 1) / kBlock - first, 0);
+        }
+        x = make_int4(b, u.kvh + (prefix ? kOfPrefix : 0), u.tile, first + pages * u.split / u.splits);
+        y = make_int4(first + pages * (u.split + 1) / u.splits, row, r.x, prefix ? more.x : more.y);
+      }
+    }
+    P.share.part[2 * i] = x;
+    P.share.part[2 * i + 1] = y;
+  }
+}
+
+// The parts of a layer: a workgroup looks its part up, and takes it as few or as many rows.
+constexpr int kWaves = 4;
+constexpr int tiles_rt(int d) { return d == 256 ? 2 : 4; }
+constexpr int tiles_qr(int d) { return d == 64 ? 4 : 2; }
+constexpr int tiles_waves(int d) { return d == 64 ? 3 : 2; }
+
+template <int D, int DT, int ROWS>
+struct Kind {                                     // tiles of ROWS rows
+  static constexpr bool kMany = ROWS == tile_rows_many(D);
+  using Few = RowsMemory<D, ROWS / 16, kWaves>;
+  using Many = TilesMemory<D, DT, tiles_rt(D), tiles_qr(D), kWaves>;
+  using Memory = std::conditional_t<kMany, Many, Few>;
+  // (own pages are read by one workgroup but for two tiles of a request at d 256)
+  template <Mode MODE>
+  __device__ static __forceinline__ void part(const CacheAttendParams& P, const Part& u, int row, int p0, int p1, Memory& memory) {
+    if constexpr (kMany) tiles_part<D, DT, tiles_rt(D), tiles_qr(D), kWaves, MODE == kOwn && D != 256, MODE>(P, u, row, p0, p1, memory);
+    else rows_part<D, DT, ROWS / 16, kWaves, MODE>(P, u, row, p0, p1, memory);
+  }
+};
+
+template <int D, int DT, int PREFIX, int OWN>
+__device__ __forceinline__ void shared_part(const CacheAttendParams& P) {
+  __shared__ union Memory {
+    typename Kind<D, DT, PREFIX>::Memory prefix;
+    typename Kind<D, DT, OWN>::Memory own;
+    typename Kind<D, DT, 16>::Memory few;
+    typename Kind<D, DT, PREFIX < 32 ? 16 : 32>::Memory some;
+    std::conditional_t<(PREFIX > 32), TilesMemory<D, DT, 2, 2, kWaves>, int> half;
+  } memory;
+  const int4 x = P.share.part[2 * blockIdx.x], y = P.share.part[2 * blockIdx.x + 1];
+  auto same = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  Part u;
+  u.b = same(x.x);
+  if (u.b < 0) return;
+  u.kvh = same(x.y);
+  u.tile = same(x.z);
+  u.q = same(y.z);
+  const int p0 = same(x.w), p1 = same(y.x), row = same(y.y), last = same(y.w);
+  if (u.kvh >= kOfPrefix) {
+    u.kvh -= kOfPrefix;
+    u.slot = last;
+    u.kv = p1 * kBlock;
+    // Few rows cost less as what they are.  A group's only tile reads bytes that no other one does: straight into
+    // registers (4 requests of 7 rows behind 128K: 35 us, 38.5 as a half tile through LDS, 40 as a tile of 64); the last one of
+    // several shares them (32 requests of 7 rows: 90, 82 and 86 us).
+    const int live = u.q * P.s.G - u.tile * PREFIX;
+    if constexpr (PREFIX > 16)
+      if (live <= 16 && u.tile == 0) return Kind<D, DT, 16>::template part<kPrefix>(P, u, row, p0, p1, memory.few);
+    if constexpr (PREFIX > 32)
+      if (live <= 32) {
+        if (u.tile == 0) return Kind<D, DT, 32>::template part<kPrefix>(P, u, row, p0, p1, memory.some);
+        u.tile *= 2;
+        return tiles_part<D, DT, 2, 2, kWaves, false, kPrefix>(P, u, row, p0, p1, memory.half);
+      }
+    Kind<D, DT, PREFIX>::template part<kPrefix>(P, u, row, p0, p1, memory.prefix);
+  } else {
+    u.kv = last;
+    Kind<D, DT, OWN>::template part<kOwn>(P, u, row, p0, p1, memory.own);
+  }
+}
+
+template <int D, int DT, int OWN>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(tiles_waves(D), tiles_waves(D))))
+shared_tiles_kernel(CacheAttendParams P) {
+  shared_part<D, DT, tile_rows_many(D), OWN>(P);
+}
+template <int D, int DT>
+__global__ void __launch_bounds__(64 * kWaves) shared_rows_kernel(CacheAttendParams P) {
+  shared_part<D, DT, 16, 16>(P);
+}
+
+template <int D, int DT>
+void shared_parts(const CacheAttendParams& P, const Sizes& z, hipStream_t stream) {
+  const unsigned n = (unsigned)z.parts;
+  if (z.prefix_rows == 16) shared_rows_kernel<D, DT><<<n, 64 * kWaves, 0, stream>>>(P);
+  else if (z.own_rows == 16) shared_tiles_kernel<D, DT, 16><<<n, 64 * kWaves, 0, stream>>>(P);
+  else if (z.own_rows == 32) shared_tiles_kernel<D, DT, 32><<<n, 64 * kWaves, 0, stream>>>(P);
+  else if constexpr (D != 256) shared_tiles_kernel<D, DT, 64><<<n, 64 * kWaves, 0, stream>>>(P);
 }
 
 // Joins the parts of the rows of a request, those of the prefix first: NT threads to a row, D / 4 to a
@@ -293,17 +451,17 @@ __global__ void __launch_bounds__(kPlanThreads) share_plan_kernel(CacheAttendPar
 template <int D, int NT>
 __global__ void __launch_bounds__(256) share_join_kernel(CacheAttendParams P, int own_rows, int prefix_rows) {
   constexpr int CG = D / 4, GR = NT / CG, ROWS = 256 / NT, W = NT / 64, kAhead = 8;
-  constexpr int kMost = 2 * (kTarget + 1);  // parts of a row
+  constexpr int kMost = kTarget / 2 * 3 + 2;        // parts of a row
   __shared__ float s_weight[ROWS][kMost];
   __shared__ float2 s_ml[4];
   __shared__ f32x4 s_o[W > 1 ? GR : 1][CG];
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, G = P.s.G;
   const int b = blockIdx.x / P.s.Hkv, kvh = blockIdx.x % P.s.Hkv, mine = tid / NT, t = tid % NT;
   const int r = blockIdx.y * ROWS + mine;
-  const int4 x = P.share.own[3 * b], y = P.share.own[3 * b + 1], z = P.share.own[3 * b + 2];
+  const int4 x = P.share.own[2 * b], y = P.share.own[2 * b + 1];
   // (a row's threads leave together: no barrier where there is a wave or less to a row)
-  if (x.z < 0 || r >= z.x * G) return;
-  const int all = (z.x * G + 15) / 16 * 16, tile = r / own_rows;
+  if (x.z < 0 || r >= x.x * G) return;
+  const int all = (x.x * G + 15) / 16 * 16, tile = r / own_rows;
   const int64_t own = (int64_t)x.z + (int64_t)x.y * (kvh * all + tile * own_rows) + r % own_rows;
   const int step = min(own_rows, all - tile * own_rows), np = y.x < 0 ? 0 : y.y;
   const int rp = y.z * G + r, tp = rp / prefix_rows;
@@ -384,10 +542,13 @@ __global__ void __launch_bounds__(256) share_join_kernel(CacheAttendParams P, in
   store_row(P, u, D, r, 4 * c, o, reciprocal(M, l));
 }
 
+// The fewer rows, the more parts of each: 112 rows of some 100 parts take 8 us with a workgroup to a row, 24 with a
+// wave; 2048 rows of 9 parts 6.3 and 4.5.
 template <int D>
 void join_shared(const CacheAttendParams& P, const Sizes& z, hipStream_t stream) {
-  const int rows = P.s.rows * P.s.G;
-  share_join_kernel<D, 256><<<dim3((unsigned)(P.s.B * P.s.Hkv), rows), 256, 0, stream>>>(P, z.own_rows, z.prefix_rows);
+  const int rows = P.s.rows * P.s.G, units = P.s.B * P.s.Hkv;
+  if (units * rows < 1024) share_join_kernel<D, 256><<<dim3(units, rows), 256, 0, stream>>>(P, z.own_rows, z.prefix_rows);
+  else share_join_kernel<D, 64><<<dim3(units, (rows + 3) / 4), 256, 0, stream>>>(P, z.own_rows, z.prefix_rows);
 }
 
 CacheAttendParams params_of(const CacheShape& s, const int32_t* table, const int32_t* kv_lens, const int32_t* q_lens) {
@@ -420,9 +581,10 @@ hipError_t launch_cache_share(const CacheShape& s, const int32_t* group, const i
   lay_out(s, share, &P.share);
   const Sizes z = sizes_of(s);
   share_compare_kernel<<<(unsigned)s.B, 256, 0, stream>>>(P, group);
-  const int64_t want = (z.own_parts + z.prefix_parts + 4 * kPlanThreads - 1) / (4 * kPlanThreads);
-  share_plan_kernel<<<(unsigned)(want < 64 ? want : 64), kPlanThreads, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.own_parts,
-                                                                                  (int)z.prefix_parts);
+  const float places = (float)places_of(s.d, z.prefix_rows);
+  if (s.B <= 256) share_plan_kernel<256, 1><<<1, 256, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
+  else if (s.B <= 1024) share_plan_kernel<1024, 1><<<1, 1024, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
+  else share_plan_kernel<1024, UGBS_MAX_REQUESTS / 1024><<<1, 1024, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
   return hipGetLastError();
 }
 
@@ -439,12 +601,10 @@ hipError_t launch_cache_attend_shared(const CacheShape& s, const uint16_t* Q, co
   const Sizes z = sizes_of(s);
   P.part_o = static_cast<float*>(workspace);
   P.part_ml = reinterpret_cast<float2*>(P.part_o + (size_t)z.sum_rows * s.d);
-  auto parts = [&](Mode mode, int rows, int64_t n, bool once) {
-    if (rows == tile_rows_many(s.d)) launch_shared_tiles(P, mode, (unsigned)n, once, stream);
-    else launch_shared_rows(P, mode, (unsigned)n, rows, stream);
-  };
-  parts(kPrefix, z.prefix_rows, z.prefix_parts, (int64_t)s.B * s.rows * s.G <= z.prefix_rows);
-  parts(kOwn, z.own_rows, z.own_parts, (int64_t)s.rows * s.G <= z.own_rows);
+  const bool f8 = s.dtype == UGBS_E4M3;
+  if (s.d == 64) (f8 ? shared_parts<64, UGBS_E4M3> : shared_parts<64, UGBS_INT8>)(P, z, stream);
+  else if (s.d == 128) (f8 ? shared_parts<128, UGBS_E4M3> : shared_parts<128, UGBS_INT8>)(P, z, stream);
+  else (f8 ? shared_parts<256, UGBS_E4M3> : shared_parts<256, UGBS_INT8>)(P, z, stream);
   if (s.d == 64) join_shared<64>(P, z, stream);
   else if (s.d == 128) join_shared<128>(P, z, stream);
   else join_shared<256>(P, z, stream);
