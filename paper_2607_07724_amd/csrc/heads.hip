@@ -6,19 +6,20 @@
 namespace ugbs {
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4, kTokenWaves = 1;
 
 template <int D, int PAIRS>
 __global__ void __launch_bounds__(64 * kWaves) heads_split_kernel(HeadsParams P, int heads_each) {
-  __shared__ __align__(16) float2 s_angle[kTokens<D> * D / 2];
+  __shared__ __align__(16) float2 s_angle[kTokenWaves * kTokens<D> * D / 2];
   const int h0 = blockIdx.y * heads_each, all = P.s.H + 2 * P.s.Hkv;
-  split_heads<D, PAIRS, kWaves>(P, blockIdx.x * kTokens<D>, h0, min(h0 + heads_each, all), s_angle);
+  split_heads<D, PAIRS, kWaves, kTokenWaves>(P, place_in_row(blockIdx.x, gridDim.x) * (kTokenWaves * kTokens<D>), h0, min(h0 + heads_each, all), s_angle);
 }
 
 template <int D, int PAIRS>
 void split(const HeadsParams& P, hipStream_t stream) {
-  const int64_t groups = ((int64_t)P.s.B * P.s.rows + kTokens<D> - 1) / kTokens<D>;
-  const int heads = P.s.H + 2 * P.s.Hkv, slices = head_slices(groups, heads, kWaves), each = (heads + slices - 1) / slices;
+  constexpr int T = kTokenWaves * kTokens<D>;
+  const int64_t groups = ((int64_t)P.s.B * P.s.rows + T - 1) / T;
+  const int heads = P.s.H + 2 * P.s.Hkv, slices = head_slices(groups, heads, kWaves / kTokenWaves), each = (heads + slices - 1) / slices;
   heads_split_kernel<D, PAIRS><<<dim3((unsigned)groups, (heads + each - 1) / each), 64 * kWaves, 0, stream>>>(P, each);
 }
 

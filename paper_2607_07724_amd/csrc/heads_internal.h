@@ -2,9 +2,10 @@
 // position, and the launchers of the kernels.
 //
 // A row is the d channels of one head of one token.  d / 16 lanes hold it, 16 channels
-// each, as two eights A and B: of the rotated channels those that the rotation pairs
-// (8 l .. 8 l + 7 with rot / 2 + 8 l .., or 16 neighbours), so a lane rotates by itself with
-// 8 angles, 8 l .. 8 l + 7; of the others 16 in a row.
+// each, as two eights, 8 l .. 8 l + 7 and as many half the rotated channels further on; the other
+// channels' likewise.  So the lanes' first eights follow each other, as do their second ones (a
+// store of every other 16 bytes costs: 15000 tokens of 16/2 heads, d 256, 66 us for 55), and a lane
+// rotates by itself, whichever way channels are paired, with 8 angles.
 //   y = x / sqrt(mean x^2 + eps) * w,   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
 // in fp32, rounded to bf16 once at the end.  Products and sums are written as the
 // operations they are (no contraction left to the compiler), so that every kernel that
@@ -78,10 +79,34 @@ __device__ __forceinline__ int rows_of(const HeadsParams& P, int b) {
 }
 
 // Where the eights of lane l of a row lie.
-template <int PAIRS>
 __device__ __forceinline__ int2 eights_of(const HeadsShape& s, int l) {
-  if (PAIRS == UGBS_HALVES && 16 * l < s.rot) return make_int2(8 * l, s.rot / 2 + 8 * l);
-  return make_int2(16 * l, 16 * l + 8);
+  const bool rotated = 16 * l < s.rot;
+  const int first = rotated ? 0 : s.rot, n = rotated ? s.rot : s.d - s.rot, at = first + 8 * (l - first / 16);    // among these n channels
+  return make_int2(at, at + n / 2);
+}
+
+// The angles of lane l, which lie in a row of rot / 2: pairs of channels c and c + rot / 2, or 2 j and 2 j + 1.
+template <int PAIRS>
+__device__ __forceinline__ void angles_of(const HeadsShape& s, const float2* row, int l, float2 (&cs)[8]) {
+  if (16 * l >= s.rot) l = 0;
+  const int second = PAIRS == UGBS_HALVES ? 8 * l + 4 : s.rot / 4 + 4 * l;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float4 y = reinterpret_cast<const float4*>(row + (e < 2 ? (PAIRS == UGBS_HALVES ? 8 * l : 4 * l) : second))[e & 1];
+    cs[2 * e] = make_float2(y.x, y.y);
+    cs[2 * e + 1] = make_float2(y.z, y.w);
+  }
+}
+
+// 16 bytes that the next kernel reads, if they are still there: nothing here does.
+__device__ __forceinline__ void store_through(uint16_t* to, uint4 v) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v), reinterpret_cast<u32x4*>(to));
+}
+
+// Workgroup j of n runs on XCD j mod 8: its place such that each XCD has a share in a row.
+__device__ __forceinline__ int place_in_row(int j, int n) {
+  const int x = j % 8, q = n / 8, r = n % 8;
+  return x * q + min(x, r) + j / 8;
 }
 
 // Sum over the LANES lanes of a row (4, 8 or 16, all active).
@@ -159,50 +184,50 @@ constexpr int kTokens = 1024 / D;
 // the work of a workgroup of NW waves.  A wave takes a head of kTokens tokens at a time, whose
 // rows follow each other in the result (1 to 2 KiB in a row).  The angles are formed once, in LDS,
 // and stay in registers over the heads.
-template <int D, int PAIRS, int NW>
+template <int D, int PAIRS, int NW, int TW>
 __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0, int h1, float2* s_angle) {
-  constexpr int LANES = D / 16, T = kTokens<D>;
+  constexpr int LANES = D / 16, T = kTokens<D>, HW = NW / TW;
   const HeadsShape& s = P.s;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane % LANES, total = s.B * s.rows, half = s.rot / 2;
-  const int n = min(n0 + lane / LANES, total - 1), b = n / s.rows, i = n % s.rows;
-  const bool live = n0 + lane / LANES < total && i < rows_of(P, b), rotated = 16 * l < s.rot;
+  const int t = w / HW * T + lane / LANES, n = min(n0 + t, total - 1), b = n / s.rows, i = n % s.rows;
+  const bool live = n0 + t < total && i < rows_of(P, b), rotated = 16 * l < s.rot;
   float2 cs[8];
   if (s.rot > 0 && h0 < s.H + s.Hkv) {
-    for (int x = tid; x < T * half; x += 64 * NW) {
-      const int t = min(n0 + x / half, total - 1);
-      s_angle[x] = angle_of(P, t / s.rows, t % s.rows, x % half);
+    for (int x = tid; x < TW * T * half; x += 64 * NW) {
+      const int at = min(n0 + x / half, total - 1);
+      s_angle[x] = angle_of(P, at / s.rows, at % s.rows, x % half);
     }
     __syncthreads();
-    const float4* const from = reinterpret_cast<const float4*>(s_angle + lane / LANES * half + (rotated ? 8 * l : 0));
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float4 y = from[e];
-      cs[2 * e] = make_float2(y.x, y.y);
-      cs[2 * e + 1] = make_float2(y.z, y.w);
-    }
+    angles_of<PAIRS>(s, s_angle + t * half, l, cs);
   }
-  const int2 c = eights_of<PAIRS>(s, l);
-  int h = h0 + w;
+  const int2 c = eights_of(s, l);
+  int h = h0 + w % HW;
   auto part = [&](const ugbs_rows& from, uint16_t* to, const float* norm, int before, int heads, bool turn) {
     if (h >= min(h1, before + heads)) return;
     float wt[16];
     if (norm) weights_of(norm, c, wt);
     const uint16_t* const x = row_at(from, b, i, 0);
     uint16_t* const y = to + ((size_t)b * heads * s.rows + i) * D;
-    for (; h < min(h1, before + heads); h += NW) {
-      uint4 u = make_uint4(0, 0, 0, 0), v = u;
-      if (live) {
-        const uint16_t* const at = x + (int64_t)(h - before) * from.head;
-        u = *reinterpret_cast<const uint4*>(at + c.x);
-        v = *reinterpret_cast<const uint4*>(at + c.y);
-      }
+    // the next head's row is on its way while this one is worked on
+    const int end = min(h1, before + heads);
+    uint4 u, v, u2 = make_uint4(0, 0, 0, 0), v2 = u2;
+    auto fetch = [&](int at_head, uint4& a, uint4& b) {
+      const uint16_t* const at = x + (int64_t)(at_head - before) * from.head;
+      a = *reinterpret_cast<const uint4*>(at + c.x);
+      b = *reinterpret_cast<const uint4*>(at + c.y);
+    };
+    if (live) fetch(h, u2, v2);
+    for (; h < end; h += HW) {
+      u = u2;
+      v = v2;
+      if (live && h + HW < end) fetch(h + HW, u2, v2);
       if (norm) do_row<D, PAIRS, true>(u, v, wt, cs, turn && rotated, s.eps);
       else if (turn) do_row<D, PAIRS, false>(u, v, wt, cs, rotated, s.eps);
       if (live) {
         uint16_t* const at = y + (size_t)(h - before) * s.rows * D;
-        *reinterpret_cast<uint4*>(at + c.x) = u;
-        *reinterpret_cast<uint4*>(at + c.y) = v;
+        store_through(at + c.x, u);
+        store_through(at + c.y, v);
       }
     }
   };

@@ -18,7 +18,7 @@ struct ProjectionRows {
   const HeadsParams& P;
   float2* s_angle;                          // [32][rot / 2]
 
-  __device__ __forceinline__ int2 eights() const { return eights_of<PAIRS>(P.s, (int)threadIdx.x % LANES); }
+  __device__ __forceinline__ int2 eights() const { return eights_of(P.s, (int)threadIdx.x % LANES); }
   __device__ __forceinline__ int key_token(int e) const { return (int)threadIdx.x / LANES + 32 * (e >> 1); }
   __device__ __forceinline__ int key_channel(int e) const { return e & 1 ? eights().y : eights().x; }
 
@@ -48,13 +48,7 @@ struct ProjectionRows {
         for (int x = (lo - 32 * r) * half + tid; x < (hi - 32 * r) * half; x += 2 * D)
           s_angle[x] = angle_of(P, b, at + 32 * r + x / half, x % half);
         __syncthreads();
-        const float4* const from = reinterpret_cast<const float4*>(s_angle + tid / LANES * half + (rotated ? 8 * l : 0));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float4 y = from[e];
-          cs[2 * e] = make_float2(y.x, y.y);
-          cs[2 * e + 1] = make_float2(y.z, y.w);
-        }
+        angles_of<PAIRS>(P.s, s_angle + tid / LANES * half, l, cs);
       }
       if (P.k_norm) do_row<D, PAIRS, true>(k[2 * r], k[2 * r + 1], wt, cs, turn && rotated, P.s.eps);
       else do_row<D, PAIRS, false>(k[2 * r], k[2 * r + 1], wt, cs, rotated, P.s.eps);
@@ -75,7 +69,7 @@ __global__ void __launch_bounds__(2 * D) heads_store_kernel(HeadsParams P, Cache
     store_page<D, DT>(c, ProjectionRows<D, PAIRS>{P, s_angle}, slots, cache, scales, pages_each, blockIdx.x, s_page);
   } else {
     const int h0 = u / groups * heads_each;
-    split_heads<D, PAIRS, 2 * D / 64>(P, u % groups * kTokens<D>, h0, min(h0 + heads_each, P.s.H), s_angle);
+    split_heads<D, PAIRS, 2 * D / 64, 1>(P, place_in_row(u % groups, groups) * kTokens<D>, h0, min(h0 + heads_each, P.s.H), s_angle);
   }
 }
 
