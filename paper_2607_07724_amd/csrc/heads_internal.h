@@ -41,13 +41,18 @@ hipError_t launch_heads_store(const HeadsParams& P, const CacheShape& c, const i
 
 namespace {
 
-// (cos, sin) of 2 pi t times gain.  t modulo a quarter turn in 64 bits leaves |y| <= 1/8;
-// cos and sin of 2 pi y by their Taylor series, which end 1e-10 and 2e-9 off at an eighth.
-__device__ __forceinline__ float2 turned(double t, float gain) {
-  const double quarters = __builtin_rint(4.0 * t);
-  const float x = (float)(__builtin_fma(-0.25, quarters, t) * 6.283185307179586);
-  // quarters mod 4 (of numbers up to 2^33, exact)
-  const int n = (int)__builtin_fma(-4.0, __builtin_floor(0.25 * quarters), quarters);
+// An angle in turns, modulo one, in units of 2^-64: what a position adds to it (whole turns that a frequency has per
+// position are whole turns at every position).
+__device__ __forceinline__ uint64_t turns_of(double f) {
+  const double t = f * 0.15915494309189535;
+  return (uint64_t)((t - __builtin_floor(t)) * 18446744073709551616.0);
+}
+
+// (cos, sin) of an angle, times gain: the nearest quarter turn, and what is left, 2 pi y with |y| <= 1/8, by the
+// Taylor series, which end 1e-10 (cos) and 2e-9 (sin) off at an eighth.
+__device__ __forceinline__ float2 turned(uint64_t turns, float gain) {
+  const uint32_t u = (uint32_t)(turns >> 32), n = (u + (1u << 29)) >> 30;
+  const float x = (float)(int)(u - (n << 30)) * 1.4629180792671596e-9f;                // 2 pi / 2^32
   const float z = x * x;
   float s = __builtin_fmaf(z, 2.7557319e-6f, -1.9841270e-4f);
   s = __builtin_fmaf(z, s, 8.3333333e-3f);
@@ -59,20 +64,40 @@ __device__ __forceinline__ float2 turned(double t, float gain) {
   c = __builtin_fmaf(z, c, -0.5f);
   c = __builtin_fmaf(z, c, 1.0f);
   const float a = n & 1 ? s : c, b = n & 1 ? c : s;
-  return make_float2((n == 1 || n == 2 ? -a : a) * gain, (n >= 2 ? -b : b) * gain);
+  return make_float2((n + 1 & 2 ? -a : a) * gain, (n & 2 ? -b : b) * gain);
 }
 
-// The angle of pair j at token i of request b.
-__device__ __forceinline__ float2 angle_of(const HeadsParams& P, int b, int i, int j) {
-  int pos;
-  if (P.positions) {
-    const int a = P.axis ? min(max(P.axis[j], 0), P.s.axes - 1) : 0;
-    pos = P.positions[((size_t)a * P.s.B + b) * P.s.rows + i];
-    return turned((double)pos * (P.freqs[j] * 0.15915494309189535), P.s.gain);
+// Angles of tokens into LDS, [token][rot / 2], by THREADS threads, each of which takes one pair of channels.
+template <int THREADS>
+struct Angles {
+  int half, j, t0, at_once, axis;
+  double f;
+  // (its loads are asked for early, and waited for when angles are formed)
+  __device__ __forceinline__ explicit Angles(const HeadsParams& P) {
+    half = P.s.rot / 2;
+    j = t0 = at_once = axis = 0;
+    f = 0.0;
+    if (half == 0) return;
+    j = (int)threadIdx.x % half;
+    t0 = (int)threadIdx.x / half;
+    at_once = THREADS / half;
+    f = P.freqs[j];
+    if (P.positions && P.axis) axis = min(max(P.axis[j], 0), P.s.axes - 1);
   }
-  const int64_t at = (int64_t)(P.first ? P.first[b] : 0) + i;
-  return turned((double)at * (P.freqs[j] * 0.15915494309189535), P.s.gain);
-}
+  // Tokens from .. behind - 1.  token(t): its request and row.
+  template <class Token>
+  __device__ __forceinline__ void fill(const HeadsParams& P, int from, int behind, Token token, float2* s_angle) const {
+    if (t0 >= at_once) return;
+    const uint64_t step = turns_of(f);
+    for (int t = from + t0; t < behind; t += at_once) {
+      const int2 x = token(t);
+      int64_t pos;
+      if (P.positions) pos = P.positions[((size_t)axis * P.s.B + x.x) * P.s.rows + x.y];
+      else pos = (int64_t)(P.first ? P.first[x.x] : 0) + x.y;
+      s_angle[t * half + j] = turned((uint64_t)pos * step, P.s.gain);
+    }
+  }
+};
 
 __device__ __forceinline__ int rows_of(const HeadsParams& P, int b) {
   return P.lens ? min(max(P.lens[b], 0), P.s.rows) : P.s.rows;
@@ -194,10 +219,10 @@ __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0
   const bool live = n0 + t < total && i < rows_of(P, b), rotated = 16 * l < s.rot;
   float2 cs[8];
   if (s.rot > 0 && h0 < s.H + s.Hkv) {
-    for (int x = tid; x < TW * T * half; x += 64 * NW) {
-      const int at = min(n0 + x / half, total - 1);
-      s_angle[x] = angle_of(P, at / s.rows, at % s.rows, x % half);
-    }
+    Angles<64 * NW>(P).fill(P, 0, TW * T, [&](int x) {
+      const int at = min(n0 + x, total - 1);
+      return make_int2(at / s.rows, at % s.rows);
+    }, s_angle);
     __syncthreads();
     angles_of<PAIRS>(s, s_angle + t * half, l, cs);
   }
