@@ -123,11 +123,6 @@ class Heads(ctypes.Structure):
                 f"rot={self.rot_dim}, pairs={'neighbours' if self.pairs == NEIGHBOURS else 'halves'}, axes={self.axes})")
 
 
-class _Rows(ctypes.Structure):
-    """Mirror of ``ugbs_rows``."""
-    _fields_ = [("at", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
-
-
 _lib = None
 
 
@@ -171,9 +166,9 @@ def lib():
         for f in ("ugbs_cache_share_bytes", "ugbs_cache_shared_workspace_bytes"):
             getattr(L, f).argtypes = [pc]
             getattr(L, f).restype = ctypes.c_size_t
-        ph, pr = ctypes.POINTER(Heads), ctypes.POINTER(_Rows)
-        L.ugbs_heads_split.argtypes = [ph, pr, pr, pr] + 11 * [P]
-        L.ugbs_heads_store.argtypes = [ph, pc, pr, pr, pr] + 12 * [P]
+        ph = ctypes.POINTER(Heads)
+        L.ugbs_heads_split.argtypes = [ph] + 14 * [P]
+        L.ugbs_heads_store.argtypes = [ph, pc] + 15 * [P]
         for f in ("ugbs_block_meta", "ugbs_score_select", "ugbs_route", "ugbs_attend", "ugbs_abi_version",
                   "ugbs_attend_select", "ugbs_select_rows", "ugbs_attend_bitmap",
                   "ugbs_noise_scale", "ugbs_bai_tiles", "ugbs_bai_heads", "ugbs_route_noalloc",
@@ -640,8 +635,8 @@ def ugbs_cache_attend_shared(c: Cache, Q, cache, scales, table, kv_lens, q_lens,
 
 # ---------------------------------------------------------------- heads
 
-def _rows_of(name, t, shape, index, dev):
-    """A tensor [B,rows,heads,d] whose last axis is contiguous, by its strides."""
+def _rows_of(name, t, shape, index):
+    """A tensor [B,rows,heads,d] whose last axis is contiguous, as the numbers of a ugbs_rows: address and strides."""
     if t is None:
         raise ValueError(f"{name} is required")
     if t.shape != shape:
@@ -649,26 +644,31 @@ def _rows_of(name, t, shape, index, dev):
     if t.dtype not in _BF16:
         raise ValueError(f"{name}: dtype {t.dtype} not in {_BF16}")
     if t.get_device() != index:
-        raise ValueError(f"{name} is on {t.device}, expected {dev}")
+        raise ValueError(f"{name} is on {t.device}, expected device {index}")
     b, i, h, c = t.stride()
     if c != 1:
         raise ValueError(f"{name}: the channels of a head must follow each other")
+    B, rows, heads, _ = shape
     # (the stride of an axis of one is anything)
-    return _Rows(t.data_ptr(), b if shape[0] > 1 else 0, i if shape[1] > 1 else 0, h if shape[2] > 1 else 0)
+    return t.data_ptr(), b if B > 1 else 0, i if rows > 1 else 0, h if heads > 1 else 0
 
 
-def _maybe(name, t, shape, dtypes, index, dev):
-    return None if t is None else _addr(name, t, shape, dtypes, index, dev)
+_Views = ctypes.c_int64 * 12            # three ugbs_rows
 
 
 def _heads_args(h, Xq, Xk, Xv, freqs, q_norm, k_norm, positions, axis, first, lens, index, dev):
-    B, H, Hkv, d, rows = h.batch, h.n_heads, h.n_kv_heads, h.head_dim, h.rows
-    kv, w, half = (B, rows, Hkv, d), (d,), (h.rot_dim // 2,)
-    return (ctypes.byref(_rows_of("Xq", Xq, (B, rows, H, d), index, dev)), ctypes.byref(_rows_of("Xk", Xk, kv, index, dev)),
-            ctypes.byref(_rows_of("Xv", Xv, kv, index, dev)), _maybe("q_norm", q_norm, w, _F32, index, dev),
-            _maybe("k_norm", k_norm, w, _F32, index, dev), _maybe("freqs", freqs, half, _F64, index, dev),
-            _maybe("positions", positions, (h.axes, B, rows), _I32, index, dev), _maybe("axis", axis, half, _I32, index, dev),
-            _maybe("first", first, (B,), _I32, index, dev), _maybe("lens", lens, (B,), _I32, index, dev))
+    B, Hkv, d, rows = h.batch, h.n_kv_heads, h.head_dim, h.rows
+    kv = (B, rows, Hkv, d)
+    views = _Views(*_rows_of("Xq", Xq, (B, rows, h.n_heads, d), index), *_rows_of("Xk", Xk, kv, index), *_rows_of("Xv", Xv, kv, index))
+    half = h.rot_dim // 2
+    return (ctypes.byref(views), ctypes.byref(views, 32), ctypes.byref(views, 64),
+            None if q_norm is None else _addr("q_norm", q_norm, (d,), _F32, index, dev),
+            None if k_norm is None else _addr("k_norm", k_norm, (d,), _F32, index, dev),
+            None if freqs is None else _addr("freqs", freqs, (half,), _F64, index, dev),
+            None if positions is None else _addr("positions", positions, (h.axes, B, rows), _I32, index, dev),
+            None if axis is None else _addr("axis", axis, (half,), _I32, index, dev),
+            None if first is None else _addr("first", first, (B,), _I32, index, dev),
+            None if lens is None else _addr("lens", lens, (B,), _I32, index, dev))
 
 
 def ugbs_heads_split(h: Heads, Xq, Xk, Xv, freqs, Q, K, V, q_norm=None, k_norm=None, positions=None, axis=None, first=None,

@@ -9,6 +9,11 @@ import paper_2607_07724_amd as ugbs
 from test_abi_cpu import _enum
 
 
+class Rows(ctypes.Structure):
+    """Mirror of ugbs_rows."""
+    _fields_ = [("at", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 def fake(i):
     return ctypes.c_void_p(0x100000 * (i + 1))        # never dereferenced: validation fails first
 
@@ -35,7 +40,7 @@ def call(store, h, c=None, null=None, off=None, stride=None, rows_null=None):
     """One call; array `null` is NULL, `off` moved by 2 bytes, rows `stride[0]` have stride[1] for field stride[2]."""
     more = ("slots", "cache", "scales") if store else ("K", "V")
     p = {n: fake(i) for i, n in enumerate(ARRAYS + more)}
-    rows = {n: ugbs._Rows(0x9000000 + 0x100000 * i, 4096, 1024, 128) for i, n in enumerate("qkv")}
+    rows = {n: Rows(0x9000000 + 0x100000 * i, 4096, 1024, 128) for i, n in enumerate("qkv")}
     if null in rows:
         rows[null].at = None
     elif null:
@@ -115,7 +120,7 @@ def test_a_cache_of_another_batch_is_refused():
 
 def test_struct_layouts_match_the_header():
     assert ctypes.sizeof(ugbs.Heads) == 40 and ugbs.Heads.norm_eps.offset == 32
-    assert ctypes.sizeof(ugbs._Rows) == 32 and ugbs._Rows.head.offset == 24
+    assert ctypes.sizeof(ugbs._Views) == 3 * ctypes.sizeof(Rows) and Rows.head.offset == 24
 
 
 def test_python_refuses_tensors_that_are_not_rows():
@@ -126,10 +131,12 @@ def test_python_refuses_tensors_that_are_not_rows():
     with pytest.raises(ValueError, match="device tensor"):
         ugbs.ugbs_heads_split(h, None, x, x, None, x, x, x)
     ugbs._get_torch()
-    cpu = (x.get_device(), x.device)
-    assert ugbs._rows_of("Xq", x, (1, 3, 2, 64), *cpu).token == 128
+    cpu = x.get_device()
+    assert ugbs._rows_of("Xq", x, (1, 3, 2, 64), cpu) == (x.data_ptr(), 0, 128, 64)
     for bad, why in ((x.transpose(1, 2), "shape"), (x.float(), "dtype"), (x[..., ::1].transpose(2, 3).contiguous().transpose(2, 3), "channels")):
         with pytest.raises(ValueError, match=why):
-            ugbs._rows_of("Xq", bad, (1, 3, 2, 64), *cpu)
+            ugbs._rows_of("Xq", bad, (1, 3, 2, 64), cpu)
     with pytest.raises(ValueError, match="required"):
-        ugbs._rows_of("Xq", None, (1, 3, 2, 64), *cpu)
+        ugbs._rows_of("Xq", None, (1, 3, 2, 64), cpu)
+    with pytest.raises(ValueError, match="is on"):
+        ugbs._rows_of("Xq", x, (1, 3, 2, 64), 0)
