@@ -164,10 +164,17 @@ constexpr float kStart = 8.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
 constexpr int kTimes = 6;                 // candidates for the longest part's time, each
 constexpr float kLonger = 0.15f;          // so much longer than the one before
 
-// The parts: the work of one workgroup, PER requests a thread.
-template <int THREADS, int PER>
-__global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P, int own_rows, int prefix_rows, int parts, float places) {
+// The parts, PER requests a thread.  PER 1: every workgroup forms the requests' entries and sums for itself, in LDS, and
+// writes its share.  More: one workgroup, which finds its entries again in the plan.  FIND: what share_compare_kernel does
+// comes first here, for few requests of few pages.
+template <int THREADS, int PER, bool FIND>
+__global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P, const int32_t* __restrict__ group, int own_rows,
+                                                             int prefix_rows, int parts, float places) {
   constexpr int NW = THREADS / 64, MOST = THREADS * PER;
+  constexpr bool kMany = PER == 1;
+  // new tokens, parts of a tile, rows of sums before, common pages; of the group the same; first entry in `row`, cached tokens
+  __shared__ int4 s_own[kMany ? MOST : 1], s_pre[kMany ? MOST : 1];
+  __shared__ int2 s_more[kMany ? MOST : 1];
   __shared__ int s_a[MOST], s_b[MOST], s_c[MOST];
   __shared__ float s_sum[4][NW], s_parts[kTimes][NW];
   __shared__ int s_scan[5][NW];
@@ -184,10 +191,38 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     found[k] = make_int4(-1, 0, 0, 0);
     own[k] = pre[k] = Lengths{0, 0, 0, 0};
     if (b < B) {
-      found[k] = P.share.found[b];
+      if constexpr (!FIND) found[k] = P.share.found[b];
       own[k].q = min(max(P.q_lens[b], 0), P.s.rows);
       own[k].kv = min(max(P.kv_lens[b], 0), most);
     }
+  }
+  if constexpr (FIND) {
+    static_assert(PER == 1, "a request a thread");
+    // (s_own: group or -1, new tokens, full pages, pages in common with the leader)
+    const int mine = tid < B && own[0].q > 0 ? group[tid] : -1;
+    s_own[tid] = make_int4(mine, own[0].q, own[0].kv / kBlock, INT32_MAX);
+    __syncthreads();
+    int members = 0, leader = -1;
+    if (mine >= 0)
+      for (int x = 0; x < B; ++x) {
+        const int4 y = s_own[x];
+        if (y.x != mine) continue;
+        if (members++ == 0) leader = x;
+        if (x < tid) found[0].z += y.y;
+      }
+    if (members > 1) {
+      found[0].x = leader;
+      s_own[tid].w = min(s_own[tid].z, s_own[leader].z);
+    }
+    s_more[tid].x = found[0].x;
+    __syncthreads();
+    const int width = P.s.max_pages;
+    for (int i = tid; i < B * width; i += THREADS) {
+      const int b = i / width, j = i - b * width, l = s_more[b].x;
+      if (l >= 0 && l != b && j < s_own[b].w && P.table[(size_t)b * width + j] != P.table[(size_t)l * width + j]) atomicMin(&s_own[b].w, j);
+    }
+    __syncthreads();
+    found[0].y = s_own[tid].w;
   }
   __syncthreads();
 #pragma unroll
@@ -240,7 +275,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     *o = *p = UGBS_MAX_BLOCKS;
     if (!P.splits) return;
     // (no more than `places` parts above the tiles, own and of prefixes together)
-    const float most = fmaxf((sums[0] + sums[1]) * each, least), x = fmaxf((time - start) / cost, most), y = fmaxf(time - kStart, most);
+    const float most = fmaxf((sums[0] + sums[1]) * each, least), x = fmaxf((time - start) * __builtin_amdgcn_rcpf(cost), most), y = fmaxf(time - kStart, most);
     *o = x < (float)UGBS_MAX_BLOCKS ? (int)x + 1 : UGBS_MAX_BLOCKS;
     *p = y < (float)UGBS_MAX_BLOCKS ? (int)y + 1 : UGBS_MAX_BLOCKS;
   };
@@ -248,8 +283,8 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
 #pragma unroll
   for (int y = 0; y < 4; ++y) {
     time = (cost * sums[0] + sums[1] + start * n_o + kStart * n_p) * each;
-    n_o = fmaxf(sums[2], sums[0] * cost / fmaxf(time - start, 1.0f));
-    n_p = fmaxf(sums[3], sums[1] / fmaxf(time - kStart, 1.0f));
+    n_o = fmaxf(sums[2], sums[0] * cost * __builtin_amdgcn_rcpf(fmaxf(time - start, 1.0f)));
+    n_p = fmaxf(sums[3], sums[1] * __builtin_amdgcn_rcpf(fmaxf(time - kStart, 1.0f)));
   }
   float longer = 1.0f;
   if (sums[2] + sums[3] <= places) {
@@ -258,7 +293,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     for (int y = 0; y < kTimes; ++y) {
       int o, p;
       pages_of_time(time * (1.0f + kLonger * y), &o, &p);
-      const float io = 1.0f / o, ip = 1.0f / p;
+      const float io = __builtin_amdgcn_rcpf((float)o), ip = __builtin_amdgcn_rcpf((float)p);
       parts_at[y] = 0.f;
 #pragma unroll
       for (int k = 0; k < PER; ++k)
@@ -299,25 +334,39 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     if (b < B) {
       s_a[b] = at[0];
       s_b[b] = at[2];
-      P.share.own[2 * b] = make_int4(own[k].q, so, so > 1 || found[k].y > 0 ? at[1] : -1, found[k].y);
-      P.share.prefix[2 * b] = make_int4(pre[k].q, sp, at[3], pre[k].pages);
-      P.share.prefix[2 * b + 1] = make_int4(at[4], own[k].kv, 0, 0);
+      const int4 o = make_int4(own[k].q, so, so > 1 || found[k].y > 0 ? at[1] : -1, found[k].y);
+      const int4 p = make_int4(pre[k].q, sp, at[3], pre[k].pages);
+      if (blockIdx.x == 0) P.share.own[2 * b] = o;
+      if constexpr (kMany) {
+        s_own[b] = o;
+        s_pre[b] = p;
+        s_more[b] = make_int2(at[4], own[k].kv);
+      } else {
+        P.share.prefix[2 * b] = p;
+        P.share.prefix[2 * b + 1] = make_int4(at[4], own[k].kv, 0, 0);
+      }
     }
 #pragma unroll
     for (int y = 0; y < 5; ++y) at[y] += x[y];
   }
   __syncthreads();
-  // the requests' entries
+  auto own_of = [&](int b) { return kMany ? s_own[kMany ? b : 0] : P.share.own[2 * b]; };
+  auto prefix_of = [&](int b) { return kMany ? s_pre[kMany ? b : 0] : P.share.prefix[2 * b]; };
+  auto more_of = [&](int b) {
+    if constexpr (kMany) return s_more[b];
+    const int4 x = P.share.prefix[2 * b + 1];
+    return make_int2(x.x, x.y);
+  };
+  // what the join and the parts of prefixes look up
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int b = PER * tid + k, l = found[k].x;
-    if (b >= B) continue;
+    if (b >= B || b % gridDim.x != blockIdx.x) continue;
     int4 y = make_int4(-1, 0, 0, 0);
     if (found[k].y > 0) {
-      const int4 of = P.share.prefix[2 * l];
-      const int map = P.share.prefix[2 * l + 1].x;
+      const int4 of = prefix_of(l);
       y = make_int4(of.z, of.y, found[k].z, (together[k] * G + 15) / 16 * 16);
-      int2* const row = P.share.row + (size_t)(map + found[k].z) * G;
+      int2* const row = P.share.row + (size_t)(more_of(l).x + found[k].z) * G;
       for (int i = 0; i < own[k].q; ++i)
         for (int g = 0; g < G; ++g) row[i * G + g] = make_int2((b * P.s.H + g) * P.s.rows + i, own[k].kv - own[k].q + i);
     }
@@ -336,14 +385,15 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   // The list: the parts of prefixes, which are longer, first.  (Spread among the others, so that each CU has
   // one of each, 64 requests behind 8K tokens took 34.6 us for 32.9.)
   const int behind = (total[2] + 7) / 8 * 8;
-  for (int i = tid; i < parts; i += THREADS) {
+  for (int i = blockIdx.x * THREADS + tid; i < parts; i += gridDim.x * THREADS) {
     int4 x = make_int4(-1, 0, 0, 0), y = x;
     if (i < behind + total[0]) {
       const bool prefix = i < behind;
       const int pos = prefix ? i : i - behind;
       if (!prefix || pos < total[2]) {
         const int b = request_at(prefix ? s_b : s_a, pos);
-        const int4 r = prefix ? P.share.prefix[2 * b] : P.share.own[2 * b], more = P.share.prefix[2 * b + 1];
+        const int4 r = prefix ? prefix_of(b) : own_of(b);
+        const int2 more = more_of(b);
         const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size, all = (rows + 15) / 16 * 16;
         Part u;
         u.splits = r.y;
@@ -580,11 +630,15 @@ hipError_t launch_cache_share(const CacheShape& s, const int32_t* group, const i
   CacheAttendParams P = params_of(s, table, kv_lens, q_lens);
   lay_out(s, share, &P.share);
   const Sizes z = sizes_of(s);
-  share_compare_kernel<<<(unsigned)s.B, 256, 0, stream>>>(P, group);
   const float places = (float)places_of(s.d, z.prefix_rows);
-  if (s.B <= 256) share_plan_kernel<256, 1><<<1, 256, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
-  else if (s.B <= 1024) share_plan_kernel<1024, 1><<<1, 1024, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
-  else share_plan_kernel<1024, UGBS_MAX_REQUESTS / 1024><<<1, 1024, 0, stream>>>(P, z.own_rows, z.prefix_rows, (int)z.parts, places);
+  const bool few = s.B <= 64 && s.B * s.max_pages <= 4096;
+  if (!few) share_compare_kernel<<<(unsigned)s.B, 256, 0, stream>>>(P, group);
+  auto blocks = [&](int threads) { return (unsigned)std::min<int64_t>((z.parts + threads - 1) / threads, 16); };
+  const int parts = (int)z.parts;
+  if (few) share_plan_kernel<256, 1, true><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
+  else if (s.B <= 256) share_plan_kernel<256, 1, false><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
+  else if (s.B <= 1024) share_plan_kernel<1024, 1, false><<<blocks(1024), 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
+  else share_plan_kernel<1024, UGBS_MAX_REQUESTS / 1024, false><<<1, 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
   return hipGetLastError();
 }
 
