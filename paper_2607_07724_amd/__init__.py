@@ -28,6 +28,7 @@ __all__ = [
     "ugbs_cache_attend", "ugbs_cache_workspace_bytes", "CacheBuffers", "CacheStep", "prefill_cached", "cache_layer",
     "HALVES", "NEIGHBOURS", "Heads", "ugbs_heads_split", "ugbs_heads_store",
     "ugbs_cache_share", "ugbs_cache_attend_shared", "ugbs_cache_share_bytes", "ugbs_cache_shared_workspace_bytes",
+    "rows_layer",
 ]
 
 KMEAN, QUEST = 0, 1
@@ -750,9 +751,9 @@ class CacheBuffers:
 class CacheStep:
     """What the layers of a step share: table, free pages, lengths, slots and the attention's workspace
     (allocated by torch).  At first all pages are free and all requests empty.  Made for the `rows` of `c`;
-    a step may be planned with fewer (single tokens after prompts)."""
+    a step may be planned with fewer (single tokens after prompts).  shared: steps may be planned with groups."""
 
-    def __init__(self, c: Cache, device="cuda"):
+    def __init__(self, c: Cache, device="cuda", shared=False):
         import torch
         i32 = dict(dtype=torch.int32, device=device)
         B = c.batch
@@ -767,16 +768,42 @@ class CacheStep:
         self.q_lens = torch.zeros((B,), **i32)
         self._slots = torch.full((B * c.rows,), -1, **i32)
         self.slots = self._slots.view(B, c.rows)
-        self.workspace = torch.empty((max(ugbs_cache_workspace_bytes(c), 256),), dtype=torch.uint8, device=device)
+        self.grouped, self.share = False, None
+        nbytes = max(ugbs_cache_workspace_bytes(c), 256)
+        if shared:
+            # the most that a step of any number of rows needs (from 64 rows of a kv head on nothing is shared)
+            fewer = [Cache.from_buffer_copy(c) for _ in range(min(c.rows, max(1, 64 // (c.n_heads // c.n_kv_heads))))]
+            for i, x in enumerate(fewer):
+                x.rows = i + 1
+            nbytes = max([nbytes] + [ugbs_cache_shared_workspace_bytes(x) for x in fewer])
+            self.share = torch.empty((max([256] + [ugbs_cache_share_bytes(x) for x in fewer]),), dtype=torch.uint8, device=device)
+        self.workspace = torch.empty((nbytes,), dtype=torch.uint8, device=device)
 
-    def plan(self, c: Cache, new_lens, stream=None):
+    def fork(self, source: int, requests, tokens: int):
+        """Requests (numbers [n], empty so far) begin with the first `tokens` tokens of request `source`, whole pages of
+        them, which they list from now on too.  Only one of a page's requests may be released with the page in its row:
+        `leave` comes first for the others."""
+        if tokens % BLOCK or not 0 <= tokens <= BLOCK * self.table.shape[1]:
+            raise ValueError(f"tokens ({tokens}) are whole pages, at most {self.table.shape[1]} of them")
+        self.table[requests, :tokens // BLOCK] = self.table[source, :tokens // BLOCK]
+        self.kv_lens[requests] = tokens
+
+    def leave(self, requests, tokens: int):
+        """Requests no longer list the pages of their first `tokens` tokens (before they are released: these pages stay
+        with the requests that go on listing them)."""
+        self.table[requests, :(tokens + BLOCK - 1) // BLOCK] = -1
+
+    def plan(self, c: Cache, new_lens, stream=None, group=None):
         """A step: every request goes on from its kv_lens with new_lens [B] int32 tokens.  Called once, before
         the step's layers, on the current stream (or `stream`, as the layers' calls).  `c` is the layers' too:
-        its `rows` give the shape of `slots`."""
+        its `rows` give the shape of `slots`.  group [B] int32: requests of equal numbers >= 0 share the first pages
+        that they have in common; the layers' attention then reads these once (of a step made with `shared`)."""
         torch = _get_torch()
         n = c.batch * c.rows
         if n > self._slots.numel():
             raise ValueError(f"the step was made for at most {self._slots.numel() // c.batch} rows, not {c.rows}")
+        if group is not None and self.share is None:
+            raise ValueError("steps with groups need CacheStep(c, shared=True)")
         self.slots = self._slots[:n].view(c.batch, c.rows)
         if stream is None:
             torch.add(self._after, 0, out=self._before)
@@ -785,8 +812,19 @@ class CacheStep:
             with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=dev) if stream
                                    else torch.cuda.default_stream(dev)):
                 torch.add(self._after, 0, out=self._before)
+        self.grouped = group is not None
         ugbs_cache_plan(c, self.ctx_lens, new_lens, self.free_pages, self.free_count, self.table, self.kv_lens,
                         self.q_lens, self.slots, self.free_left, stream)
+        if self.grouped:
+            ugbs_cache_share(c, group, self.table, self.kv_lens, self.q_lens, self.share, stream)
+
+    def attend(self, c: Cache, Q, O, cbufs: CacheBuffers, stream=None):
+        """A layer's attention of the step's tokens, whose keys and values are in the cache."""
+        if self.grouped:
+            ugbs_cache_attend_shared(c, Q, cbufs.cache, cbufs.scales, self.table, self.kv_lens, self.q_lens, self.share, O,
+                                     self.workspace, stream)
+        else:
+            ugbs_cache_attend(c, Q, cbufs.cache, cbufs.scales, self.table, self.kv_lens, self.q_lens, O, self.workspace, stream)
 
 
 def prefill_cached(p: Problem, c: Cache, Q, K, V, O, bufs: Buffers, cbufs: CacheBuffers, step: CacheStep, stream=None):
@@ -803,7 +841,17 @@ def prefill_cached(p: Problem, c: Cache, Q, K, V, O, bufs: Buffers, cbufs: Cache
 def cache_layer(c: Cache, Q, K, V, O, cbufs: CacheBuffers, step: CacheStep, stream=None):
     """One layer of a step: the new tokens' K and V into the cache, then their attention over all of it."""
     ugbs_cache_store(c, K, V, step.slots, cbufs.cache, cbufs.scales, stream)
-    ugbs_cache_attend(c, Q, cbufs.cache, cbufs.scales, step.table, step.kv_lens, step.q_lens, O, step.workspace, stream)
+    step.attend(c, Q, O, cbufs, stream)
+    return O
+
+
+def rows_layer(h: Heads, c: Cache, Xq, Xk, Xv, freqs, Q, O, cbufs: CacheBuffers, step: CacheStep, q_norm=None, k_norm=None,
+               positions=None, axis=None, stream=None):
+    """cache_layer from a projection's rows (ugbs_heads_store; Q [B,H,rows,d] is scratch).  Without positions the tokens follow
+    the requests' cached ones."""
+    ugbs_heads_store(h, c, Xq, Xk, Xv, freqs, Q, step.slots, cbufs.cache, cbufs.scales, q_norm, k_norm, positions, axis,
+                     None if positions is not None else step.ctx_lens, step.q_lens, stream)
+    step.attend(c, Q, O, cbufs, stream)
     return O
 
 
