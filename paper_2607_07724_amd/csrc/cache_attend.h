@@ -29,8 +29,7 @@ struct Schedule {
 
 // Where the parts lie of a batch whose requests list common first pages: formed once a step by
 // ugbs_cache_share.  A group of such requests has a leader, its first one.  The rows of a part's sums
-// lie in the workspace one behind another, a tile's rows rounded up to 16: part `split` of tile t, kv
-// head h of rows R in all (R a multiple of 16) begins at row
+// lie in the workspace one behind another: part `split` of tile t of kv head h, R rows in all, begins at row
 //   before + splits (h R + t ROWS) + split min(ROWS, R - t ROWS).
 struct Share {
   int4* own;          // [B][2]: (new tokens, parts of a tile, rows before or -1: written to O, common pages),

@@ -49,7 +49,7 @@ Sizes sizes_of(const CacheShape& s) {
   z.prefix_rows = prefix_tile_rows(s.d, all);
   const int more = places_of(s.d, z.prefix_rows);
   z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + more + 8;
-  z.sum_rows = s.Hkv * (s.B * (((int64_t)s.rows * s.G + 15) / 16 * 16) + all + 15 * groups) + more * std::max(z.own_rows, z.prefix_rows);
+  z.sum_rows = 2 * s.Hkv * all + more * std::max(z.own_rows, z.prefix_rows);
   return z;
 }
 
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   __shared__ int4 s_own[kMany ? MOST : 1], s_pre[kMany ? MOST : 1];
   __shared__ int2 s_more[kMany ? MOST : 1];
   __shared__ int s_a[MOST], s_b[MOST], s_c[MOST];
-  __shared__ float s_sum[4][NW], s_parts[kTimes][NW];
+  __shared__ float s_sum[5][NW], s_parts[kTimes][NW];
   __shared__ int s_scan[5][NW];
   const int tid = threadIdx.x, B = P.s.B, G = P.s.G, Hkv = P.s.Hkv, most = P.s.max_pages * kBlock;
   for (int b = tid; b < B; b += THREADS) {
@@ -256,7 +256,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   }
   // Pages a part, from the time that the longest may take: all parts together, spread evenly over the chip's
   // places, and longer until there is a place for each (where there are more tiles than places: as it is).
-  float sums[4] = {0.f, 0.f, 0.f, 0.f};                        // work and tiles, own and of prefixes
+  float sums[5] = {0.f, 0.f, 0.f, 0.f, 0.f};                   // work and tiles, own and of prefixes; pages of all tiles
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     sums[0] = __builtin_fmaf((float)own[k].tiles, (float)own[k].pages, sums[0]);
@@ -265,17 +265,18 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     sums[1] = __builtin_fmaf((float)pre[k].tiles - few, (float)pre[k].pages, sums[1]);
     sums[2] += (float)own[k].tiles;
     sums[3] += (float)pre[k].tiles;
+    sums[4] += (float)(own[k].tiles * own[k].pages + pre[k].tiles * pre[k].pages);
   }
   sum_all<NW>(sums, s_sum);
 #pragma unroll
-  for (int y = 0; y < 4; ++y) sums[y] *= (float)Hkv;
+  for (int y = 0; y < 5; ++y) sums[y] *= (float)Hkv;
   const bool alike = own_rows == prefix_rows;
   const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart, least = (float)P.min_pages, each = 1.0f / places;
   auto pages_of_time = [&](float time, int* o, int* p) {
     *o = *p = UGBS_MAX_BLOCKS;
     if (!P.splits) return;
     // (no more than `places` parts above the tiles, own and of prefixes together)
-    const float most = fmaxf((sums[0] + sums[1]) * each, least), x = fmaxf((time - start) * __builtin_amdgcn_rcpf(cost), most), y = fmaxf(time - kStart, most);
+    const float most = fmaxf(sums[4] * each, least), x = fmaxf((time - start) * __builtin_amdgcn_rcpf(cost), most), y = fmaxf(time - kStart, most);
     *o = x < (float)UGBS_MAX_BLOCKS ? (int)x + 1 : UGBS_MAX_BLOCKS;
     *p = y < (float)UGBS_MAX_BLOCKS ? (int)y + 1 : UGBS_MAX_BLOCKS;
   };
@@ -311,9 +312,9 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   auto count = [&](int k, int (&x)[5]) {
     const int so = splits_of(own[k], per_own), sp = splits_of(pre[k], per_pre);
     x[0] = own[k].tiles * Hkv * so;
-    x[1] = own[k].tiles > 0 && (so > 1 || found[k].y > 0) ? so * Hkv * ((own[k].q * G + 15) / 16 * 16) : 0;
+    x[1] = own[k].tiles > 0 && (so > 1 || found[k].y > 0) ? so * Hkv * own[k].q * G : 0;
     x[2] = pre[k].tiles * Hkv * sp;
-    x[3] = sp * Hkv * ((pre[k].q * G + 15) / 16 * 16);
+    x[3] = sp * Hkv * pre[k].q * G;
     x[4] = pre[k].q;
   };
 #pragma unroll
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     int4 y = make_int4(-1, 0, 0, 0);
     if (found[k].y > 0) {
       const int4 of = prefix_of(l);
-      y = make_int4(of.z, of.y, found[k].z, (together[k] * G + 15) / 16 * 16);
+      y = make_int4(of.z, of.y, found[k].z, together[k] * G);
       int2* const row = P.share.row + (size_t)(more_of(l).x + found[k].z) * G;
       for (int i = 0; i < own[k].q; ++i)
         for (int g = 0; g < G; ++g) row[i * G + g] = make_int2((b * P.s.H + g) * P.s.rows + i, own[k].kv - own[k].q + i);
@@ -394,12 +395,12 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
         const int b = request_at(prefix ? s_b : s_a, pos);
         const int4 r = prefix ? prefix_of(b) : own_of(b);
         const int2 more = more_of(b);
-        const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size, all = (rows + 15) / 16 * 16;
+        const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size;
         Part u;
         u.splits = r.y;
         if (prefix) locate<kGroups>(P, pos - s_b[b], tiles, 0, &u);
         else locate<kParts>(P, pos - s_a[b], tiles, 0, &u);
-        const int row = r.z < 0 ? -1 : r.z + u.splits * (u.kvh * all + u.tile * size) + u.split * min(size, all - u.tile * size);
+        const int row = r.z < 0 ? -1 : r.z + u.splits * (u.kvh * rows + u.tile * size) + u.split * min(size, rows - u.tile * size);
         int first = 0, pages = r.w;
         if (!prefix) {
           // pages that the tile's last row sees, behind the common ones
@@ -511,7 +512,7 @@ __global__ void __launch_bounds__(256) share_join_kernel(CacheAttendParams P, in
   const int4 x = P.share.own[2 * b], y = P.share.own[2 * b + 1];
   // (a row's threads leave together: no barrier where there is a wave or less to a row)
   if (x.z < 0 || r >= x.x * G) return;
-  const int all = (x.x * G + 15) / 16 * 16, tile = r / own_rows;
+  const int all = x.x * G, tile = r / own_rows;
   const int64_t own = (int64_t)x.z + (int64_t)x.y * (kvh * all + tile * own_rows) + r % own_rows;
   const int step = min(own_rows, all - tile * own_rows), np = y.x < 0 ? 0 : y.y;
   const int rp = y.z * G + r, tp = rp / prefix_rows;
