@@ -160,7 +160,7 @@ __device__ __forceinline__ void sum_before(const int (&x)[N], int (&before)[N], 
 }
 
 // What a part costs, in pages of a prefix part: its start and end; a page and the start of a part of own pages.
-constexpr float kStart = 8.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
+constexpr float kStart = 6.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
 constexpr int kTimes = 6;                 // candidates for the longest part's time, each
 constexpr float kLonger = 0.15f;          // so much longer than the one before
 
@@ -280,13 +280,17 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     *o = x < (float)UGBS_MAX_BLOCKS ? (int)x + 1 : UGBS_MAX_BLOCKS;
     *p = y < (float)UGBS_MAX_BLOCKS ? (int)y + 1 : UGBS_MAX_BLOCKS;
   };
-  float time = 0.f, n_o = sums[2], n_p = sums[3];
+  // (x pages of a prefix in the longest part: time(x) = a + b / x, whose fixed point the geometric mean of both approaches
+  // from one side)
+  float x = fmaxf((cost * sums[0] + sums[1]) * each, 1.0f);
 #pragma unroll
-  for (int y = 0; y < 4; ++y) {
-    time = (cost * sums[0] + sums[1] + start * n_o + kStart * n_p) * each;
-    n_o = fmaxf(sums[2], sums[0] * cost * __builtin_amdgcn_rcpf(fmaxf(time - start, 1.0f)));
-    n_p = fmaxf(sums[3], sums[1] * __builtin_amdgcn_rcpf(fmaxf(time - kStart, 1.0f)));
+  for (int y = 0; y < 6; ++y) {
+    const float n_o = fmaxf(sums[2], sums[0] * cost * __builtin_amdgcn_rcpf(fmaxf(x + kStart - start, 1.0f)));
+    const float n_p = fmaxf(sums[3], sums[1] * __builtin_amdgcn_rcpf(x));
+    const float t = (cost * sums[0] + sums[1] + start * n_o + kStart * n_p) * each - kStart;
+    x = fmaxf(__builtin_amdgcn_sqrtf(x * fmaxf(t, 1.0f)), 1.0f);
   }
+  const float time = x + kStart;
   float longer = 1.0f;
   if (sums[2] + sums[3] <= places) {
     float parts_at[kTimes];
