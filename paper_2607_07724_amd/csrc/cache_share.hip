@@ -38,18 +38,14 @@ struct Sizes {
 // tile of 64 is bound by the same bytes).
 int prefix_tile_rows(int d, int64_t rows) { return rows <= 16 ? 16 : tile_rows_many(d); }
 
-// Workgroups that the chip holds at once (two a CU, three with the small tiles of d 64).
-int places_of(int d, int prefix_rows) { return d == 64 && prefix_rows != 16 ? kTarget / 2 * 3 : kTarget; }
-
-// More parts than tiles: by `places` at most; a group has two requests at least.
+// More parts than tiles: by kTarget at most; a group has two requests at least.
 Sizes sizes_of(const CacheShape& s) {
   const int64_t all = (int64_t)s.B * s.rows * s.G, groups = s.B / 2;
   Sizes z;
   z.own_rows = tile_rows(s);
   z.prefix_rows = prefix_tile_rows(s.d, all);
-  const int more = places_of(s.d, z.prefix_rows);
-  z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + more + 8;
-  z.sum_rows = 2 * s.Hkv * all + more * std::max(z.own_rows, z.prefix_rows);
+    z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + kTarget + 8;
+  z.sum_rows = 2 * s.Hkv * all + kTarget * std::max(z.own_rows, z.prefix_rows);
   return z;
 }
 
@@ -161,15 +157,15 @@ __device__ __forceinline__ void sum_before(const int (&x)[N], int (&before)[N], 
 
 // What a part costs, in pages of a prefix part: its start and end; a page and the start of a part of own pages.
 constexpr float kStart = 6.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
-constexpr int kTimes = 6;                 // candidates for the longest part's time, each
-constexpr float kLonger = 0.15f;          // so much longer than the one before
+constexpr int kTimes = 8;                 // candidates for the longest part's time, each
+constexpr float kLonger = 0.1f;           // so much longer than the one before
 
 // The parts, PER requests a thread.  PER 1: every workgroup forms the requests' entries and sums for itself, in LDS, and
 // writes its share.  More: one workgroup, which finds its entries again in the plan.  FIND: what share_compare_kernel does
 // comes first here, for few requests of few pages.
 template <int THREADS, int PER, bool FIND>
 __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P, const int32_t* __restrict__ group, int own_rows,
-                                                             int prefix_rows, int parts, float places) {
+                                                             int prefix_rows, int parts) {
   constexpr int NW = THREADS / 64, MOST = THREADS * PER;
   constexpr bool kMany = PER == 1;
   // new tokens, parts of a tile, rows of sums before, common pages; of the group the same; first entry in `row`, cached tokens
@@ -271,11 +267,11 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
 #pragma unroll
   for (int y = 0; y < 5; ++y) sums[y] *= (float)Hkv;
   const bool alike = own_rows == prefix_rows;
-  const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart, least = (float)P.min_pages, each = 1.0f / places;
+  const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart, least = (float)P.min_pages, each = 1.0f / kTarget;
   auto pages_of_time = [&](float time, int* o, int* p) {
     *o = *p = UGBS_MAX_BLOCKS;
     if (!P.splits) return;
-    // (no more than `places` parts above the tiles, own and of prefixes together)
+    // (no more than kTarget parts above the tiles, own and of prefixes together)
     const float most = fmaxf(sums[4] * each, least), x = fmaxf((time - start) * __builtin_amdgcn_rcpf(cost), most), y = fmaxf(time - kStart, most);
     *o = x < (float)UGBS_MAX_BLOCKS ? (int)x + 1 : UGBS_MAX_BLOCKS;
     *p = y < (float)UGBS_MAX_BLOCKS ? (int)y + 1 : UGBS_MAX_BLOCKS;
@@ -292,7 +288,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   }
   const float time = x + kStart;
   float longer = 1.0f;
-  if (sums[2] + sums[3] <= places) {
+  if (sums[2] + sums[3] <= (float)kTarget) {
     float parts_at[kTimes];
 #pragma unroll
     for (int y = 0; y < kTimes; ++y) {
@@ -307,7 +303,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     sum_all<NW>(parts_at, s_parts);
 #pragma unroll
     for (int y = kTimes - 1; y >= 0; --y)
-      if (parts_at[y] * (float)Hkv <= places) longer = 1.0f + kLonger * y;
+      if (parts_at[y] * (float)Hkv <= (float)kTarget) longer = 1.0f + kLonger * y;
   }
   int per_own, per_pre;
   pages_of_time(time * longer, &per_own, &per_pre);
@@ -433,10 +429,10 @@ struct Kind {                                     // tiles of ROWS rows
   using Few = RowsMemory<D, ROWS / 16, kWaves>;
   using Many = TilesMemory<D, DT, tiles_rt(D), tiles_qr(D), kWaves>;
   using Memory = std::conditional_t<kMany, Many, Few>;
-  // (own pages are read by one workgroup but for two tiles of a request at d 256)
-  template <Mode MODE>
+  // ONCE: no other workgroup reads these bytes
+  template <Mode MODE, bool ONCE>
   __device__ static __forceinline__ void part(const CacheAttendParams& P, const Part& u, int row, int p0, int p1, Memory& memory) {
-    if constexpr (kMany) tiles_part<D, DT, tiles_rt(D), tiles_qr(D), kWaves, MODE == kOwn && D != 256, MODE>(P, u, row, p0, p1, memory);
+    if constexpr (kMany) tiles_part<D, DT, tiles_rt(D), tiles_qr(D), kWaves, ONCE, MODE>(P, u, row, p0, p1, memory);
     else rows_part<D, DT, ROWS / 16, kWaves, MODE>(P, u, row, p0, p1, memory);
   }
 };
@@ -468,17 +464,20 @@ __device__ __forceinline__ void shared_part(const CacheAttendParams& P) {
     // several shares them (32 requests of 7 rows: 90, 82 and 86 us).
     const int live = u.q * P.s.G - u.tile * PREFIX;
     if constexpr (PREFIX > 16)
-      if (live <= 16 && u.tile == 0) return Kind<D, DT, 16>::template part<kPrefix>(P, u, row, p0, p1, memory.few);
+      if (live <= 16 && u.tile == 0) return Kind<D, DT, 16>::template part<kPrefix, true>(P, u, row, p0, p1, memory.few);
     if constexpr (PREFIX > 32)
       if (live <= 32) {
-        if (u.tile == 0) return Kind<D, DT, 32>::template part<kPrefix>(P, u, row, p0, p1, memory.some);
+        if (u.tile == 0) return Kind<D, DT, 32>::template part<kPrefix, true>(P, u, row, p0, p1, memory.some);
         u.tile *= 2;
         return tiles_part<D, DT, 2, 2, kWaves, false, kPrefix>(P, u, row, p0, p1, memory.half);
       }
-    Kind<D, DT, PREFIX>::template part<kPrefix>(P, u, row, p0, p1, memory.prefix);
+    // (8 requests of 7 rows behind 128K: 39 us for 44 with the bytes kept in the caches)
+    if (live == u.q * P.s.G) Kind<D, DT, PREFIX>::template part<kPrefix, true>(P, u, row, p0, p1, memory.prefix);
+    else Kind<D, DT, PREFIX>::template part<kPrefix, false>(P, u, row, p0, p1, memory.prefix);
   } else {
     u.kv = last;
-    Kind<D, DT, OWN>::template part<kOwn>(P, u, row, p0, p1, memory.own);
+    // (own pages, but for the two tiles of a request of 33 rows and more at d 256)
+    Kind<D, DT, OWN>::template part<kOwn, D != 256>(P, u, row, p0, p1, memory.own);
   }
 }
 
@@ -506,7 +505,7 @@ void shared_parts(const CacheAttendParams& P, const Sizes& z, hipStream_t stream
 template <int D, int NT>
 __global__ void __launch_bounds__(256) share_join_kernel(CacheAttendParams P, int own_rows, int prefix_rows) {
   constexpr int CG = D / 4, GR = NT / CG, ROWS = 256 / NT, W = NT / 64, kAhead = 8;
-  constexpr int kMost = kTarget / 2 * 3 + 2;        // parts of a row
+  constexpr int kMost = kTarget + 2;        // parts of a row
   __shared__ float s_weight[ROWS][kMost];
   __shared__ float2 s_ml[4];
   __shared__ f32x4 s_o[W > 1 ? GR : 1][CG];
@@ -635,15 +634,14 @@ hipError_t launch_cache_share(const CacheShape& s, const int32_t* group, const i
   CacheAttendParams P = params_of(s, table, kv_lens, q_lens);
   lay_out(s, share, &P.share);
   const Sizes z = sizes_of(s);
-  const float places = (float)places_of(s.d, z.prefix_rows);
   const bool few = s.B <= 64 && s.B * s.max_pages <= 4096;
   if (!few) share_compare_kernel<<<(unsigned)s.B, 256, 0, stream>>>(P, group);
   auto blocks = [&](int threads) { return (unsigned)std::min<int64_t>((z.parts + threads - 1) / threads, 16); };
   const int parts = (int)z.parts;
-  if (few) share_plan_kernel<256, 1, true><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
-  else if (s.B <= 256) share_plan_kernel<256, 1, false><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
-  else if (s.B <= 1024) share_plan_kernel<1024, 1, false><<<blocks(1024), 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
-  else share_plan_kernel<1024, UGBS_MAX_REQUESTS / 1024, false><<<1, 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts, places);
+  if (few) share_plan_kernel<256, 1, true><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts);
+  else if (s.B <= 256) share_plan_kernel<256, 1, false><<<blocks(256), 256, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts);
+  else if (s.B <= 1024) share_plan_kernel<1024, 1, false><<<blocks(1024), 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts);
+  else share_plan_kernel<1024, UGBS_MAX_REQUESTS / 1024, false><<<1, 1024, 0, stream>>>(P, group, z.own_rows, z.prefix_rows, parts);
   return hipGetLastError();
 }
 

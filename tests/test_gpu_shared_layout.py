@@ -119,4 +119,4 @@ def test_one_long_prefix_uses_the_chip(B, H, Hkv, d, mp):
     kv = np.full(B, 64 * mp - 7, I32)
     parts = check(c, np.zeros(B, I32), table, kv, np.ones(B, I32))
     prefix = parts[parts[:, 1] >= OF_PREFIX]
-    assert prefix[:, 4].max() == mp - 2 and 100 <= len(prefix) <= 768
+    assert prefix[:, 4].max() == mp - 2 and 100 <= len(prefix) <= 520
