@@ -289,21 +289,29 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   const float time = x + kStart;
   float longer = 1.0f;
   if (sums[2] + sums[3] <= (float)kTarget) {
-    float parts_at[kTimes];
+    // the first of kTimes candidates with a place for each part: `from`, `from` + step, ... (else the last one)
+    auto fitting = [&](float from, float step) {
+      float parts_at[kTimes];
 #pragma unroll
-    for (int y = 0; y < kTimes; ++y) {
-      int o, p;
-      pages_of_time(time * (1.0f + kLonger * y), &o, &p);
-      const float io = __builtin_amdgcn_rcpf((float)o), ip = __builtin_amdgcn_rcpf((float)p);
-      parts_at[y] = 0.f;
+      for (int y = 0; y < kTimes; ++y) {
+        int o, p;
+        pages_of_time(time * (from + step * y), &o, &p);
+        const float io = __builtin_amdgcn_rcpf((float)o), ip = __builtin_amdgcn_rcpf((float)p);
+        parts_at[y] = 0.f;
 #pragma unroll
-      for (int k = 0; k < PER; ++k)
-        parts_at[y] += own[k].tiles * fmaxf(ceilf(own[k].pages * io), 1.0f) + pre[k].tiles * fmaxf(ceilf(pre[k].pages * ip), 1.0f);
-    }
-    sum_all<NW>(parts_at, s_parts);
+        for (int k = 0; k < PER; ++k)
+          parts_at[y] += own[k].tiles * fmaxf(ceilf(own[k].pages * io), 1.0f) + pre[k].tiles * fmaxf(ceilf(pre[k].pages * ip), 1.0f);
+      }
+      __syncthreads();
+      sum_all<NW>(parts_at, s_parts);
+      float found = from + step * (kTimes - 1);
 #pragma unroll
-    for (int y = kTimes - 1; y >= 0; --y)
-      if (parts_at[y] * (float)Hkv <= (float)kTarget) longer = 1.0f + kLonger * y;
+      for (int y = kTimes - 2; y >= 0; --y)
+        if (parts_at[y] * (float)Hkv <= (float)kTarget) found = from + step * y;
+      return found;
+    };
+    longer = fitting(1.0f, kLonger);
+    if (longer > 1.0f) longer = fitting(longer - kLonger, kLonger / (kTimes - 1));
   }
   int per_own, per_pre;
   pages_of_time(time * longer, &per_own, &per_pre);
