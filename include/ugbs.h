@@ -573,7 +573,8 @@ UGBS_API size_t ugbs_cache_workspace_bytes(const ugbs_cache* c);
  *   group   : [B] int32: requests of equal numbers >= 0 are a group; negative: alone.  What a
  *             group shares are the first entries that the table rows of all its requests
  *             with new tokens have in common, as far as these pages are full for all of them.
- *             Requests that turn out to have nothing in common cost nothing, and no answer depends on group.
+ *             Where that saves less than it costs (few common pages), and where there is nothing, the
+ *             requests are laid out alone.  No answer depends on group.
  *   table, kv_lens, q_lens : the step's.
  *   share   : device memory of at least ugbs_cache_share_bytes(c) bytes, 256-byte aligned,
  *             contents ignored; holds the layout until the next call. */
@@ -585,7 +586,7 @@ UGBS_API int ugbs_cache_share(const ugbs_cache* c, const int32_t* group, const i
  *   workspace : at least ugbs_cache_shared_workspace_bytes(c) bytes, else as for ugbs_cache_attend.
  *   For common pages the rows of all requests count together, batch rows H / H_kv, where
  *   ugbs_cache_attend takes a query channel as two e4m3 numbers.
- *   Where rows H / H_kv > 64 (pieces of prompts), each request's rows fill tiles of their own,
+ *   Where rows H / H_kv > 128 (pieces of prompts), each request's rows fill tiles of their own,
  *   bound by the matrix cores; there, with one request and with batch rows H > 2^20 nothing is
  *   shared and the call is ugbs_cache_attend. */
 UGBS_API int ugbs_cache_attend_shared(const ugbs_cache* c, const void* Q, const void* cache, const float* scales,

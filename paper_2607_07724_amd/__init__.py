@@ -771,8 +771,8 @@ class CacheStep:
         self.grouped, self.share = False, None
         nbytes = max(ugbs_cache_workspace_bytes(c), 256)
         if shared:
-            # the most that a step of any number of rows needs (from 64 rows of a kv head on nothing is shared)
-            fewer = [Cache.from_buffer_copy(c) for _ in range(min(c.rows, max(1, 64 // (c.n_heads // c.n_kv_heads))))]
+            # the most that a step of any number of rows needs (above 128 rows of a kv head nothing is shared)
+            fewer = [Cache.from_buffer_copy(c) for _ in range(min(c.rows, max(1, 128 // (c.n_heads // c.n_kv_heads))))]
             for i, x in enumerate(fewer):
                 x.rows = i + 1
             nbytes = max([nbytes] + [ugbs_cache_shared_workspace_bytes(x) for x in fewer])

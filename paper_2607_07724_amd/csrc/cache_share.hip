@@ -18,10 +18,9 @@
 namespace ugbs {
 namespace {
 
-// A group shares its common pages from this many saved page reads of a kv head on.
-constexpr int kLeastSaved = 1;
-// More query rows to a kv head than this fill a tile by themselves.
-constexpr int kMostRows = 64;
+// More query rows of a request to a kv head than this fill their tiles (8 requests behind 8K tokens: of 80 rows 44 us alone,
+// 36 together, of 128 rows 47.7 and 46.0).
+constexpr int kMostRows = 128;
 
 // (the join's grid: a workgroup for each row)
 bool shares(const CacheShape& s) {
@@ -157,6 +156,11 @@ __device__ __forceinline__ void sum_before(const int (&x)[N], int (&before)[N], 
 
 // What a part costs, in pages of a prefix part: its start and end; a page and the start of a part of own pages.
 constexpr float kStart = 6.0f, kOwnPage = 0.75f, kOwnStart = 4.0f;
+// Common pages are shared where that saves more pages a place than the rows' joins cost.  Without: 32 requests of up to 1000
+// tokens behind 4 common pages (1.4 saved) 13.6 us, with 17.5; behind 16 (5.5) 17.6 and 18.7; 8 groups of 8 behind up to 64 each
+// (23) 43.5 and 24.  Tiles that are the same for own pages save the bytes that several would read (kSameTile for 1): 8 requests of
+// 64 rows behind 128 pages (4.0) 32.5 and 30.9.
+constexpr float kSameTile = 1.25f, kLeastSaved = 7.0f, kLeastSame = 3.0f;
 constexpr int kTimes = 8;                 // candidates for the longest part's time, each
 constexpr float kLonger = 0.1f;           // so much longer than the one before
 
@@ -172,7 +176,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   __shared__ int4 s_own[kMany ? MOST : 1], s_pre[kMany ? MOST : 1];
   __shared__ int2 s_more[kMany ? MOST : 1];
   __shared__ int s_a[MOST], s_b[MOST], s_c[MOST];
-  __shared__ float s_sum[5][NW], s_parts[kTimes][NW];
+  __shared__ float s_saved[1][NW], s_sum[5][NW], s_parts[kTimes][NW];
   __shared__ int s_scan[5][NW];
   const int tid = threadIdx.x, B = P.s.B, G = P.s.G, Hkv = P.s.Hkv, most = P.s.max_pages * kBlock;
   for (int b = tid; b < B; b += THREADS) {
@@ -231,34 +235,46 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     }
   }
   __syncthreads();
+  const bool alike = own_rows == prefix_rows;
+  const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart;
+  // (the last tile of a group may be one of few rows)
+  auto prefix_work = [&](const Lengths& r) {
+    const float few = prefix_rows > 32 && r.q * G - (r.tiles - 1) * prefix_rows <= 32 ? 1.0f - kOwnPage : 0.0f;
+    return ((float)r.tiles - few) * (float)r.pages;
+  };
   int together[PER];                                           // new tokens of the group
+  float saved[1] = {0.f};
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     const int b = PER * tid + k, l = found[k].x;
-    together[k] = 0;
-    int pages = 0;
-    if (l >= 0 && s_a[l] * (s_c[l] - 1) >= kLeastSaved) {
-      pages = s_a[l];
-      together[k] = s_b[l];
-    }
-    found[k].y = pages;
+    together[k] = l >= 0 ? s_b[l] : 0;
+    found[k].y = l >= 0 ? s_a[l] : 0;
     own[k].tiles = (own[k].q * G + own_rows - 1) / own_rows;
-    own[k].pages = max((own[k].kv + kBlock - 1) / kBlock - pages, 0);
-    if (pages > 0 && b == l) {
+    saved[0] += (alike ? kSameTile : kOwnPage) * (float)(own[k].tiles * found[k].y);
+    if (found[k].y > 0 && b == l) {
       pre[k].q = together[k];
       pre[k].tiles = (together[k] * G + prefix_rows - 1) / prefix_rows;
-      pre[k].pages = pages;
+      pre[k].pages = found[k].y;
+      saved[0] -= prefix_work(pre[k]);
     }
   }
+  sum_all<NW>(saved, s_saved);
+  if (saved[0] * (float)Hkv < (float)kTarget * (prefix_rows == 16 ? 0.0f : alike ? kLeastSame : kLeastSaved)) {
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      found[k].y = 0;
+      pre[k] = Lengths{0, 0, 0, 0};
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < PER; ++k) own[k].pages = max((own[k].kv + kBlock - 1) / kBlock - found[k].y, 0);
   // Pages a part, from the time that the longest may take: all parts together, spread evenly over the chip's
   // places, and longer until there is a place for each (where there are more tiles than places: as it is).
   float sums[5] = {0.f, 0.f, 0.f, 0.f, 0.f};                   // work and tiles, own and of prefixes; pages of all tiles
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
     sums[0] = __builtin_fmaf((float)own[k].tiles, (float)own[k].pages, sums[0]);
-    // (the last tile of a group may be one of few rows)
-    const float few = prefix_rows > 32 && pre[k].q * G - (pre[k].tiles - 1) * prefix_rows <= 32 ? 1.0f - kOwnPage : 0.0f;
-    sums[1] = __builtin_fmaf((float)pre[k].tiles - few, (float)pre[k].pages, sums[1]);
+    sums[1] += prefix_work(pre[k]);
     sums[2] += (float)own[k].tiles;
     sums[3] += (float)pre[k].tiles;
     sums[4] += (float)(own[k].tiles * own[k].pages + pre[k].tiles * pre[k].pages);
@@ -266,8 +282,7 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
   sum_all<NW>(sums, s_sum);
 #pragma unroll
   for (int y = 0; y < 5; ++y) sums[y] *= (float)Hkv;
-  const bool alike = own_rows == prefix_rows;
-  const float cost = alike ? 1.0f : kOwnPage, start = alike ? kStart : kOwnStart, least = (float)P.min_pages, each = 1.0f / kTarget;
+  const float least = (float)P.min_pages, each = 1.0f / kTarget;
   auto pages_of_time = [&](float time, int* o, int* p) {
     *o = *p = UGBS_MAX_BLOCKS;
     if (!P.splits) return;
@@ -484,8 +499,9 @@ __device__ __forceinline__ void shared_part(const CacheAttendParams& P) {
     else Kind<D, DT, PREFIX>::template part<kPrefix, false>(P, u, row, p0, p1, memory.prefix);
   } else {
     u.kv = last;
-    // (own pages, but for the two tiles of a request of 33 rows and more at d 256)
-    Kind<D, DT, OWN>::template part<kOwn, D != 256>(P, u, row, p0, p1, memory.own);
+    // (tiles of many rows stay in the caches: a request may have several, and one alone is no slower, 27.2 us for 28.5 with
+    // 8 requests of 64 rows and up to 8000 tokens)
+    Kind<D, DT, OWN>::template part<kOwn, false>(P, u, row, p0, p1, memory.own);
   }
 }
 

@@ -61,5 +61,5 @@ def test_sizes_hold_the_sums_of_every_row(B, H, Hkv, d, rows):
     assert ws >= 2 * B * H * rows * (4 * d + 8)
     assert ws <= (2 * B * H * rows + 512 * 64) * (4 * d + 8)
     # rows that fill tiles of their own: the plain call's workspace
-    many = ugbs.Cache.make(B, H, Hkv, d, 1000, 100, rows=64 * Hkv // H + 1)
+    many = ugbs.Cache.make(B, H, Hkv, d, 1000, 100, rows=128 * Hkv // H + 1)
     assert ugbs.ugbs_cache_shared_workspace_bytes(many) == ugbs.ugbs_cache_workspace_bytes(many)
