@@ -582,7 +582,8 @@ UGBS_API int ugbs_cache_share(const ugbs_cache* c, const int32_t* group, const i
                               const int32_t* q_lens, void* share, size_t share_bytes, void* stream);
 
 /* ugbs_cache_attend over a layout.
- *   table, kv_lens, q_lens, share : those of the ugbs_cache_share call, which comes before on the stream.
+ *   table, kv_lens, q_lens, share : those of the ugbs_cache_share call, which comes before on the stream,
+ *             with a c of the same batch, heads, head_dim, max_pages and rows.
  *   workspace : at least ugbs_cache_shared_workspace_bytes(c) bytes, else as for ugbs_cache_attend.
  *   For common pages the rows of all requests count together, batch rows H / H_kv, where
  *   ugbs_cache_attend takes a query channel as two e4m3 numbers.

@@ -768,7 +768,7 @@ class CacheStep:
         self.q_lens = torch.zeros((B,), **i32)
         self._slots = torch.full((B * c.rows,), -1, **i32)
         self.slots = self._slots.view(B, c.rows)
-        self.grouped, self.share = False, None
+        self.grouped, self.share, self._laid_out = False, None, None
         nbytes = max(ugbs_cache_workspace_bytes(c), 256)
         if shared:
             # the most that a step of any number of rows needs (above 128 rows of a kv head nothing is shared)
@@ -781,7 +781,7 @@ class CacheStep:
 
     def fork(self, source: int, requests, tokens: int):
         """Requests (numbers [n], empty so far) begin with the first `tokens` tokens of request `source`, whole pages of
-        them, which they list from now on too.  Only one of a page's requests may be released with the page in its row:
+        them, which they list from now on too (on torch's current stream, as `leave`).  Only one of a page's requests may be released with the page in its row:
         `leave` comes first for the others."""
         if tokens % BLOCK or not 0 <= tokens <= BLOCK * self.table.shape[1]:
             raise ValueError(f"tokens ({tokens}) are whole pages, at most {self.table.shape[1]} of them")
@@ -816,11 +816,18 @@ class CacheStep:
         ugbs_cache_plan(c, self.ctx_lens, new_lens, self.free_pages, self.free_count, self.table, self.kv_lens,
                         self.q_lens, self.slots, self.free_left, stream)
         if self.grouped:
+            self._laid_out = self._layout_of(c)
             ugbs_cache_share(c, group, self.table, self.kv_lens, self.q_lens, self.share, stream)
+
+    @staticmethod
+    def _layout_of(c):
+        return c.batch, c.n_heads, c.n_kv_heads, c.head_dim, c.max_pages, c.rows
 
     def attend(self, c: Cache, Q, O, cbufs: CacheBuffers, stream=None):
         """A layer's attention of the step's tokens, whose keys and values are in the cache."""
         if self.grouped:
+            if self._layout_of(c) != self._laid_out:
+                raise ValueError(f"the step was laid out for another cache than {c}")
             ugbs_cache_attend_shared(c, Q, cbufs.cache, cbufs.scales, self.table, self.kv_lens, self.q_lens, self.share, O,
                                      self.workspace, stream)
         else:

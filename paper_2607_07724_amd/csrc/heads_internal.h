@@ -4,7 +4,7 @@
 // A row is the d channels of one head of one token.  d / 16 lanes hold it, 16 channels
 // each, as two eights, 8 l .. 8 l + 7 and as many half the rotated channels further on; the other
 // channels' likewise.  So the lanes' first eights follow each other, as do their second ones (a
-// store of every other 16 bytes costs: 15000 tokens of 16/2 heads, d 256, 66 us for 55), and a lane
+// store of every other 16 bytes costs: 15000 tokens of 16/2 heads, d 256, 66 us for 57), and a lane
 // rotates by itself, whichever way channels are paired, with 8 angles.
 //   y = x / sqrt(mean x^2 + eps) * w,   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
 // in fp32, rounded to bf16 once at the end.  Products and sums are written as the
@@ -44,8 +44,7 @@ namespace {
 // An angle in turns, modulo one, in units of 2^-64: what a position adds to it (whole turns that a frequency has per
 // position are whole turns at every position).
 __device__ __forceinline__ uint64_t turns_of(double f) {
-  const double t = f * 0.15915494309189535;
-  return (uint64_t)((t - __builtin_floor(t)) * 18446744073709551616.0);
+  return (uint64_t)(__builtin_amdgcn_fract(f * 0.15915494309189535) * 18446744073709551616.0);      // (fract is below one)
 }
 
 // (cos, sin) of an angle, times gain: the nearest quarter turn, and what is left, 2 pi y with |y| <= 1/8, by the
@@ -209,17 +208,17 @@ constexpr int kTokens = 1024 / D;
 // the work of a workgroup of NW waves.  A wave takes a head of kTokens tokens at a time, whose
 // rows follow each other in the result (1 to 2 KiB in a row).  The angles are formed once, in LDS,
 // and stay in registers over the heads.
-template <int D, int PAIRS, int NW, int TW>
+template <int D, int PAIRS, int NW>
 __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0, int h1, float2* s_angle) {
-  constexpr int LANES = D / 16, T = kTokens<D>, HW = NW / TW;
+  constexpr int LANES = D / 16, T = kTokens<D>;
   const HeadsShape& s = P.s;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l = lane % LANES, total = s.B * s.rows, half = s.rot / 2;
-  const int t = w / HW * T + lane / LANES, n = min(n0 + t, total - 1), b = n / s.rows, i = n % s.rows;
+  const int t = lane / LANES, n = min(n0 + t, total - 1), b = n / s.rows, i = n % s.rows;
   const bool live = n0 + t < total && i < rows_of(P, b), rotated = 16 * l < s.rot;
   float2 cs[8];
   if (s.rot > 0 && h0 < s.H + s.Hkv) {
-    Angles<64 * NW>(P).fill(P, 0, TW * T, [&](int x) {
+    Angles<64 * NW>(P).fill(P, 0, T, [&](int x) {
       const int at = min(n0 + x, total - 1);
       return make_int2(at / s.rows, at % s.rows);
     }, s_angle);
@@ -227,7 +226,7 @@ __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0
     angles_of<PAIRS>(s, s_angle + t * half, l, cs);
   }
   const int2 c = eights_of(s, l);
-  int h = h0 + w % HW;
+  int h = h0 + w;
   auto part = [&](const ugbs_rows& from, uint16_t* to, const float* norm, int before, int heads, bool turn) {
     if (h >= min(h1, before + heads)) return;
     float wt[16];
@@ -243,10 +242,10 @@ __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0
       b = *reinterpret_cast<const uint4*>(at + c.y);
     };
     if (live) fetch(h, u2, v2);
-    for (; h < end; h += HW) {
+    for (; h < end; h += NW) {
       u = u2;
       v = v2;
-      if (live && h + HW < end) fetch(h + HW, u2, v2);
+      if (live && h + NW < end) fetch(h + NW, u2, v2);
       if (norm) do_row<D, PAIRS, true>(u, v, wt, cs, turn && rotated, s.eps);
       else if (turn) do_row<D, PAIRS, false>(u, v, wt, cs, rotated, s.eps);
       if (live) {
@@ -262,9 +261,11 @@ __device__ __forceinline__ void split_heads(const HeadsParams& P, int n0, int h0
   part(P.v, P.V, nullptr, s.H + s.Hkv, s.Hkv, false);
 }
 
-// Workgroups along the heads: one head a wave where tokens are few.
+// Workgroups along the heads, up to one head a wave: as many as make 1024 in all, four a CU, since each slice forms
+// the angles again.  (48 heads of d 128: 500 tokens 4.3 us, at 512 in all 4.7; 2000 tokens 10.3, at 4096 11.4; 8000 tokens
+// in one slice 38, in two 40.)
 inline int head_slices(int64_t groups, int heads, int waves) {
-  const int64_t most = (heads + waves - 1) / waves, want = (1024 + groups - 1) / groups;
+  const int64_t most = (heads + waves - 1) / waves, want = groups < 1024 ? 1024 / groups : 1;
   return (int)(want < most ? want : most);
 }
 

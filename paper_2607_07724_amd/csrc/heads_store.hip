@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(2 * D) heads_store_kernel(HeadsParams P, Cache
     if (u < stores) store_page<D, DT>(c, ProjectionRows<D, PAIRS>{P, s_angle, Angles<2 * D>(P)}, slots, cache, scales, pages_each, u, s_page);
   } else {
     const int u = 8 * (e - before) + blockIdx.x % 8, h0 = u / groups * heads_each;
-    if (h0 < P.s.H) split_heads<D, PAIRS, 2 * D / 64, 1>(P, place_in_row(u % groups, groups) * kTokens<D>, h0, min(h0 + heads_each, P.s.H), s_angle);
+    if (h0 < P.s.H) split_heads<D, PAIRS, 2 * D / 64>(P, place_in_row(u % groups, groups) * kTokens<D>, h0, min(h0 + heads_each, P.s.H), s_angle);
   }
 }
 

@@ -213,6 +213,21 @@ def test_requests_of_several_tiles(rows, H, Hkv, d, dtype):
     check(g, lens, [rows] * 11 + [1, rows - 1, 0], rows, H, Hkv, d, dtype, [0] * 13 + [-1], {0: 160})
 
 
+@pytest.mark.parametrize("B,H,Hkv,rows,d,shared", [(4, 4, 1, 1, 64, True), (20, 16, 16, 1, 128, True), (70, 8, 8, 1, 128, True), (24, 28, 4, 2, 64, False),
+                                                   (72, 8, 8, 1, 64, True), (40, 16, 8, 4, 256, True)])
+def test_a_request_whose_queries_are_not_finite_leaves_its_group_alone(B, H, Hkv, rows, d, shared):
+    g = np.random.default_rng(B)
+    lens = [40 * PAGE + rows + int(g.integers(0, 200)) for _ in range(B)]
+    x = shared_contents(g, lens, Hkv, d, 0, [0] * B, {0: 40})
+    Qb, Qv = bf16(g.normal(0, 1, (B, H, rows, d)))
+    Qb[1], Qb[B // 2] = 0x7FC0, 0x7F80
+    c = ugbs.Cache.make(B, H, Hkv, d, x.n_pages, x.max_pages, rows=rows)
+    got = bf16_to_f64(host_bits(run_shared(c, x, Qb, lens, [rows] * B, [0] * B, shared=shared)))
+    for b in sorted(set(range(B)) - {1, B // 2}):
+        want, tol = reference(x, b, Qv[b], lens[b], rows, 1 / math.sqrt(d), B * rows * H // Hkv > (32 if d < 256 else 16))
+        assert (np.abs(got[b] - want) <= tol).all(), b
+
+
 def test_lengths_outside_their_range_are_clamped():
     g = np.random.default_rng(9)
     x = shared_contents(g, [640, 640, 640], 2, 64, 0, [0] * 3, {0: 8})

@@ -143,3 +143,14 @@ def test_groups_need_a_step_made_for_them_and_forks_whole_pages():
     for tokens in (1, 65, -64, 64 * 5):
         with pytest.raises(ValueError, match="whole pages"):
             step.fork(0, [1], tokens)
+
+
+def test_layers_of_another_shape_than_the_steps_layout_are_refused():
+    c, other = ugbs.Cache.make(2, 4, 1, 64, 8, 4, rows=2), ugbs.Cache.make(2, 4, 1, 64, 8, 4, rows=1)
+    step, cb = ugbs.CacheStep(c, shared=True), ugbs.CacheBuffers(c)
+    step.plan(c, dev(np.ones(2, I32)), group=dev(np.zeros(2, I32)))
+    Q = torch.zeros((2, 4, 1, 64), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError, match="another cache"):
+        step.attend(other, Q, torch.empty_like(Q), cb)
+    step.plan(other, dev(np.ones(2, I32)))                    # without groups there is no layout
+    step.attend(other, Q, torch.empty_like(Q), cb)
