@@ -46,7 +46,7 @@ Sizes sizes_of(const CacheShape& s) {
   Sizes z;
   z.own_rows = tile_rows(s);
   z.prefix_rows = prefix_tile_rows(s.d, all);
-  z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + kTarget + 8;
+  z.parts = tiles_bound(s, z.own_rows) + s.Hkv * (all / z.prefix_rows + groups) + kTarget;
   z.sum_rows = 2 * s.Hkv * all + kTarget * std::max(z.own_rows, z.prefix_rows);
   return z;
 }
@@ -410,33 +410,32 @@ __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P
     return lo;
   };
   // The list: the parts of prefixes, which are longer, first.  (Spread among the others, so that each CU has
-  // one of each, 64 requests behind 8K tokens took 34.6 us for 32.9.)
-  const int behind = (total[2] + 7) / 8 * 8;
+  // one of each, 64 requests behind 8K tokens took 34.6 us for 32.9.)  Without gaps: kTarget parts are as many for each
+  // XCD.  (With own parts from a multiple of 8 on, one XCD had 65 for its 64 places, and the last one waited for another's
+  // end: 40 drafts of d 256 behind 5 prompts 69 us for 58.)
   for (int i = blockIdx.x * THREADS + tid; i < parts; i += gridDim.x * THREADS) {
     int4 x = make_int4(-1, 0, 0, 0), y = x;
-    if (i < behind + total[0]) {
-      const bool prefix = i < behind;
-      const int pos = prefix ? i : i - behind;
-      if (!prefix || pos < total[2]) {
-        const int b = request_at(prefix ? s_b : s_a, pos);
-        const int4 r = prefix ? prefix_of(b) : own_of(b);
-        const int2 more = more_of(b);
-        const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size;
-        Part u;
-        u.splits = r.y;
-        if (prefix) locate<kGroups>(P, pos - s_b[b], tiles, 0, &u);
-        else locate<kParts>(P, pos - s_a[b], tiles, 0, &u);
-        const int row = r.z < 0 ? -1 : r.z + u.splits * (u.kvh * rows + u.tile * size) + u.split * min(size, rows - u.tile * size);
-        int first = 0, pages = r.w;
-        if (!prefix) {
-          // pages that the tile's last row sees, behind the common ones
-          const int end = more.y - r.x + (min((u.tile + 1) * size, rows) - 1) / G + 1;
-          first = r.w;
-          pages = max((max(end, 0) + kBlock - 1) / kBlock - first, 0);
-        }
-        x = make_int4(b, u.kvh + (prefix ? kOfPrefix : 0), u.tile, first + pages * u.split / u.splits);
-        y = make_int4(first + pages * (u.split + 1) / u.splits, row, r.x, prefix ? more.x : more.y);
+    if (i < total[2] + total[0]) {
+      const bool prefix = i < total[2];
+      const int pos = prefix ? i : i - total[2];
+      const int b = request_at(prefix ? s_b : s_a, pos);
+      const int4 r = prefix ? prefix_of(b) : own_of(b);
+      const int2 more = more_of(b);
+      const int size = prefix ? prefix_rows : own_rows, rows = r.x * G, tiles = (rows + size - 1) / size;
+      Part u;
+      u.splits = r.y;
+      if (prefix) locate<kGroups>(P, pos - s_b[b], tiles, 0, &u);
+      else locate<kParts>(P, pos - s_a[b], tiles, 0, &u);
+      const int row = r.z < 0 ? -1 : r.z + u.splits * (u.kvh * rows + u.tile * size) + u.split * min(size, rows - u.tile * size);
+      int first = 0, pages = r.w;
+      if (!prefix) {
+        // pages that the tile's last row sees, behind the common ones
+        const int end = more.y - r.x + (min((u.tile + 1) * size, rows) - 1) / G + 1;
+        first = r.w;
+        pages = max((max(end, 0) + kBlock - 1) / kBlock - first, 0);
       }
+      x = make_int4(b, u.kvh + (prefix ? kOfPrefix : 0), u.tile, first + pages * u.split / u.splits);
+      y = make_int4(first + pages * (u.split + 1) / u.splits, row, r.x, prefix ? more.x : more.y);
     }
     P.share.part[2 * i] = x;
     P.share.part[2 * i + 1] = y;
