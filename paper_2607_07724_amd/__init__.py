@@ -779,14 +779,37 @@ class CacheStep:
             self.share = torch.empty((max([256] + [ugbs_cache_share_bytes(x) for x in fewer]),), dtype=torch.uint8, device=device)
         self.workspace = torch.empty((nbytes,), dtype=torch.uint8, device=device)
 
+    def _listed(self, requests):
+        """[B] bool on the device: the requests that `requests` (an index of torch's into [B]) names.  Numbers that are on the
+        device already are not looked at on the host: those outside -B .. B-1 name none."""
+        torch = _get_torch()
+        B, dev = self.table.shape[0], self.table.device
+        if not (torch.is_tensor(requests) and requests.is_cuda):
+            requests = torch.arange(B)[requests].to(dev)
+        if requests.dtype == torch.bool:
+            return requests
+        x = requests.reshape(-1).long()
+        x = torch.where((x >= -B) & (x < B), x.remainder(B), B)
+        return torch.zeros(B + 1, dtype=torch.bool, device=dev).index_fill_(0, x, True)[:B]
+
     def fork(self, source: int, requests, tokens: int):
-        """Requests (numbers [n], empty so far) begin with the first `tokens` tokens of request `source`, whole pages of
-        them, which they list from now on too (on torch's current stream, as `leave`).  Only one of a page's requests may be released with the page in its row:
-        `leave` comes first for the others."""
+        """Requests (numbers [n]) that are empty begin with the first `tokens` tokens of request `source`, whole pages of
+        them, which they list from now on too (between steps, on torch's current stream, as `leave`).  Where the source has
+        fewer, they begin with those of its pages that are full; requests that have tokens of their own stay as they are.
+        Only one of a page's requests may be released with the page in its row: `leave` comes first for the others."""
         if tokens % BLOCK or not 0 <= tokens <= BLOCK * self.table.shape[1]:
             raise ValueError(f"tokens ({tokens}) are whole pages, at most {self.table.shape[1]} of them")
-        self.table[requests, :tokens // BLOCK] = self.table[source, :tokens // BLOCK]
-        self.kv_lens[requests] = tokens
+        torch = _get_torch()
+        n = tokens // BLOCK
+        mine = self._listed(requests) & (self.kv_lens == 0)
+        row = self.table[source, :n]
+        # on the device: the source's full pages, as far as it lists them
+        full = BLOCK * torch.arange(1, n + 1, device=row.device) <= self.kv_lens[source]
+        listed = (full & (row >= 0) & (row < self.free_pages.numel())).int().cumprod(0)
+        held = listed.sum()
+        row = torch.where(listed > 0, row, -1)
+        self.table[:, :n] = torch.where(mine[:, None], row, self.table[:, :n])
+        self.kv_lens.copy_(torch.where(mine, BLOCK * held.int(), self.kv_lens))
 
     def leave(self, requests, tokens: int):
         """Requests no longer list the pages of their first `tokens` tokens (before they are released: these pages stay

@@ -1,0 +1,72 @@
+"""The host's side of steps over the cache, without a GPU: forks, requests that leave pages, steps that are refused."""
+import pytest
+import torch
+
+import paper_2607_07724_amd as ugbs
+
+B = 6
+
+
+def made(kv, width=5):
+    """A step whose requests have these lengths; request b lists pages 10 b, 10 b + 1, .. to the end of its row (as after a
+    release: entries behind a request's tokens are left over)."""
+    step = ugbs.CacheStep(ugbs.Cache.make(B, 4, 1, 64, 100, width), device="cpu", shared=True)
+    step.table[:] = 10 * torch.arange(B)[:, None] + torch.arange(width)
+    step.kv_lens[:] = torch.tensor(kv)
+    return step
+
+
+def row(b, n):
+    return [10 * b + j for j in range(n)]
+
+
+def test_forks_begin_with_the_pages_that_they_ask_for():
+    step = made([200, 0, 0, 70, 0, 0])
+    step.fork(0, [1, 4], 128)
+    assert step.kv_lens.tolist() == [200, 128, 0, 70, 128, 0]
+    assert step.table[1].tolist() == row(0, 2) + [12, 13, 14] and step.table[4, :2].tolist() == row(0, 2)
+    assert step.table[0].tolist() == row(0, 5) and step.table[2].tolist() == row(2, 5)
+
+
+@pytest.mark.parametrize("have,asked,full", [(200, 256, 3), (200, 320, 3), (63, 64, 0), (0, 128, 0), (128, 128, 2), (192, 0, 0)])
+def test_a_fork_takes_no_more_than_the_full_pages_of_its_source(have, asked, full):
+    step = made([have, 0, 0, 9, 9, 9])
+    step.fork(0, [1, 2], asked)
+    assert step.kv_lens.tolist() == [have, 64 * full, 64 * full, 9, 9, 9]
+    for b in (1, 2):
+        # (what lies behind may be another request's page by now)
+        assert step.table[b, :asked // 64].tolist() == row(0, full) + [-1] * (asked // 64 - full)
+
+
+def test_pages_that_the_source_no_longer_lists_are_not_forked():
+    step = made([300, 0, 0, 0, 0, 0])
+    for none in (-1, 100):
+        step.table[0, 2] = none
+        step.kv_lens[1] = 0
+        step.fork(0, [1], 256)
+        assert step.kv_lens.tolist() == [300, 128, 0, 0, 0, 0] and step.table[1, :4].tolist() == row(0, 2) + [-1, -1]
+
+
+def test_requests_with_tokens_of_their_own_are_not_forked():
+    step = made([200, 64, 0, 5, 0, 0])
+    step.fork(0, [0, 1, 2, 3], 192)                       # the source among them
+    assert step.kv_lens.tolist() == [200, 64, 192, 5, 0, 0]
+    assert [step.table[b].tolist() for b in (0, 1, 3)] == [row(b, 5) for b in (0, 1, 3)]
+
+
+@pytest.mark.parametrize("requests", [2, [2], [2, 2], [-4], torch.tensor([2, 2]), torch.arange(B) == 2, slice(2, 3)])
+def test_requests_are_named_as_torch_takes_them(requests):
+    step = made([200, 0, 0, 0, 0, 0])
+    step.fork(0, requests, 64)
+    assert step.kv_lens.tolist() == [200, 0, 64, 0, 0, 0]
+
+
+def test_requests_that_are_none_are_refused():
+    step = made([200, 0, 0, 0, 0, 0])
+    for bad in ([6], [1, -7], torch.tensor([99])):
+        with pytest.raises(IndexError):
+            step.fork(0, bad, 64)
+    for source in (6, -7):
+        with pytest.raises(IndexError):
+            step.fork(source, [1], 64)
+    assert step.kv_lens.tolist() == [200, 0, 0, 0, 0, 0]
