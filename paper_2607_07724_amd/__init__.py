@@ -792,13 +792,16 @@ class CacheStep:
         x = torch.where((x >= -B) & (x < B), x.remainder(B), B)
         return torch.zeros(B + 1, dtype=torch.bool, device=dev).index_fill_(0, x, True)[:B]
 
+    def _whole_pages(self, tokens):
+        if tokens % BLOCK or not 0 <= tokens <= BLOCK * self.table.shape[1]:
+            raise ValueError(f"tokens ({tokens}) are whole pages, at most {self.table.shape[1]} of them")
+
     def fork(self, source: int, requests, tokens: int):
         """Requests (numbers [n]) that are empty begin with the first `tokens` tokens of request `source`, whole pages of
         them, which they list from now on too (between steps, on torch's current stream, as `leave`).  Where the source has
         fewer, they begin with those of its pages that are full; requests that have tokens of their own stay as they are.
         Only one of a page's requests may be released with the page in its row: `leave` comes first for the others."""
-        if tokens % BLOCK or not 0 <= tokens <= BLOCK * self.table.shape[1]:
-            raise ValueError(f"tokens ({tokens}) are whole pages, at most {self.table.shape[1]} of them")
+        self._whole_pages(tokens)
         torch = _get_torch()
         n = tokens // BLOCK
         mine = self._listed(requests) & (self.kv_lens == 0)
@@ -812,9 +815,11 @@ class CacheStep:
         self.kv_lens.copy_(torch.where(mine, BLOCK * held.int(), self.kv_lens))
 
     def leave(self, requests, tokens: int):
-        """Requests no longer list the pages of their first `tokens` tokens (before they are released: these pages stay
-        with the requests that go on listing them)."""
-        self.table[requests, :(tokens + BLOCK - 1) // BLOCK] = -1
+        """Requests no longer list the pages of their first `tokens` tokens, whole pages (before they are released: these
+        pages stay with the requests that go on listing them).  No more of them than other requests list: a page that nobody
+        lists any more does not come back."""
+        self._whole_pages(tokens)
+        self.table[:, :tokens // BLOCK].masked_fill_(self._listed(requests)[:, None], -1)
 
     def plan(self, c: Cache, new_lens, stream=None, group=None):
         """A step: every request goes on from its kv_lens with new_lens [B] int32 tokens.  Called once, before

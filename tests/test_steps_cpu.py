@@ -70,3 +70,32 @@ def test_requests_that_are_none_are_refused():
         with pytest.raises(IndexError):
             step.fork(source, [1], 64)
     assert step.kv_lens.tolist() == [200, 0, 0, 0, 0, 0]
+
+
+@pytest.mark.parametrize("tokens", [1, 63, 65, 200, -1, -64, -200, 64 * 6])
+def test_requests_leave_whole_pages_of_their_rows(tokens):
+    """A page that is left in part is the request's own: it would never come back to the free ones."""
+    step = made([200, 200, 0, 0, 0, 0])
+    before = step.table.clone()
+    with pytest.raises(ValueError, match="whole pages"):
+        step.leave([1], tokens)
+    assert torch.equal(step.table, before)
+
+
+@pytest.mark.parametrize("requests", [[1, 3], [3, 1, 3], torch.tensor([1, -3]), slice(1, 4, 2)])
+def test_requests_leave_what_they_have_in_common(requests):
+    step = made([200] * B)
+    step.leave(requests, 128)
+    for b in range(B):
+        assert step.table[b].tolist() == ([-1, -1] + row(b, 5)[2:] if b in (1, 3) else row(b, 5))
+    step.leave(requests, 0)
+    step.leave(requests, 64 * 5)
+    assert (step.table[[1, 3]] == -1).all() and step.table[0].tolist() == row(0, 5)
+
+
+def test_leaving_requests_that_are_none_is_refused():
+    step = made([200] * B)
+    for bad in ([6], [1, -7]):
+        with pytest.raises(IndexError):
+            step.leave(bad, 64)
+    assert (step.table >= 0).all()
