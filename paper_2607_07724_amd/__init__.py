@@ -830,9 +830,15 @@ class CacheStep:
         n = c.batch * c.rows
         if n > self._slots.numel():
             raise ValueError(f"the step was made for at most {self._slots.numel() // c.batch} rows, not {c.rows}")
-        if group is not None and self.share is None:
-            raise ValueError("steps with groups need CacheStep(c, shared=True)")
-        self.slots = self._slots[:n].view(c.batch, c.rows)
+        if group is not None:
+            # all that the layout may be refused for, before anything is planned
+            if self.share is None:
+                raise ValueError("steps with groups need CacheStep(c, shared=True)")
+            _check("group", group, (c.batch,), _I32, self.table.device)
+            if self._layout_of(c) != self._laid_out and (ugbs_cache_share_bytes(c) > self.share.nbytes or
+                                                         ugbs_cache_shared_workspace_bytes(c) > self.workspace.nbytes):
+                raise ValueError(f"the step was made for fewer heads or channels than {c}")
+        slots = self._slots[:n].view(c.batch, c.rows)
         if stream is None:
             torch.add(self._after, 0, out=self._before)
         else:
@@ -840,12 +846,12 @@ class CacheStep:
             with torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=dev) if stream
                                    else torch.cuda.default_stream(dev)):
                 torch.add(self._after, 0, out=self._before)
-        self.grouped = group is not None
         ugbs_cache_plan(c, self.ctx_lens, new_lens, self.free_pages, self.free_count, self.table, self.kv_lens,
-                        self.q_lens, self.slots, self.free_left, stream)
-        if self.grouped:
-            self._laid_out = self._layout_of(c)
+                        self.q_lens, slots, self.free_left, stream)
+        self.slots, self.grouped = slots, False
+        if group is not None:
             ugbs_cache_share(c, group, self.table, self.kv_lens, self.q_lens, self.share, stream)
+            self.grouped, self._laid_out = True, self._layout_of(c)
 
     @staticmethod
     def _layout_of(c):

@@ -99,3 +99,34 @@ def test_leaving_requests_that_are_none_is_refused():
         with pytest.raises(IndexError):
             step.leave(bad, 64)
     assert (step.table >= 0).all()
+
+
+def planned_calls(monkeypatch):
+    calls = []
+    monkeypatch.setattr(ugbs, "ugbs_cache_plan", lambda *a, **k: calls.append("plan"))
+    monkeypatch.setattr(ugbs, "ugbs_cache_share", lambda *a, **k: calls.append("share"))
+    return calls
+
+
+@pytest.mark.parametrize("group,why", [
+    (torch.zeros(B, dtype=torch.int64), "dtype"), (torch.zeros(B + 1, dtype=torch.int32), "shape"),
+    (torch.zeros((B, 1), dtype=torch.int32), "shape"), (torch.zeros(B, dtype=torch.int32), "device tensor")])
+def test_a_step_whose_groups_are_refused_is_not_planned(group, why, monkeypatch):
+    """The tokens of a step that was planned and then refused would be counted again by the next one."""
+    step, calls = made([200, 0, 64, 0, 0, 0]), planned_calls(monkeypatch)
+    step._before.fill_(7)
+    with pytest.raises(ValueError, match=why):
+        step.plan(ugbs.Cache.make(B, 4, 1, 64, 100, 5), torch.ones(B, dtype=torch.int32), group=group)
+    assert calls == [] and not step.grouped and (step._before == 7).all()
+
+
+@pytest.mark.parametrize("H,d", [(16, 64), (4, 256)])
+def test_a_step_whose_layout_does_not_fit_is_not_planned(H, d, monkeypatch):
+    """Of more query heads than the step was made for (its layout is longer), or of more channels (its workspace is)."""
+    step, calls = made([200, 0, 64, 0, 0, 0]), planned_calls(monkeypatch)
+    monkeypatch.setattr(ugbs, "_check", lambda name, t, *a: t.data_ptr())          # (no device here)
+    with pytest.raises(ValueError, match="made for"):
+        step.plan(ugbs.Cache.make(B, H, 1, d, 100, 5), torch.ones(B, dtype=torch.int32), group=torch.zeros(B, dtype=torch.int32))
+    assert calls == []
+    step.plan(ugbs.Cache.make(B, 4, 1, 64, 100, 5), torch.ones(B, dtype=torch.int32), group=torch.zeros(B, dtype=torch.int32))
+    assert calls == ["plan", "share"] and step.grouped
