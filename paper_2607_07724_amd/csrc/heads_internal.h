@@ -42,9 +42,11 @@ hipError_t launch_heads_store(const HeadsParams& P, const CacheShape& c, const i
 namespace {
 
 // An angle in turns, modulo one, in units of 2^-64: what a position adds to it (whole turns that a frequency has per
-// position are whole turns at every position).
+// position are whole turns at every position).  Of a negative one the turns are those of its opposite, backwards: the
+// fraction itself would lie just below one, where 53 bits leave 2^-54 of a turn at each position.
 __device__ __forceinline__ uint64_t turns_of(double f) {
-  return (uint64_t)(__builtin_amdgcn_fract(f * 0.15915494309189535) * 18446744073709551616.0);      // (fract is below one)
+  const uint64_t t = (uint64_t)(__builtin_amdgcn_fract(fabs(f) * 0.15915494309189535) * 18446744073709551616.0);      // (fract is below one)
+  return f < 0.0 ? 0 - t : t;
 }
 
 // (cos, sin) of an angle, times gain: the nearest quarter turn, and what is left, 2 pi y with |y| <= 1/8, by the
