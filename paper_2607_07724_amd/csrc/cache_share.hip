@@ -496,8 +496,10 @@ __device__ __forceinline__ void shared_part(const CacheAttendParams& P) {
         u.tile *= 2;
         return tiles_part<D, DT, 2, 2, kWaves, false, kPrefix>(P, u, row, p0, p1, memory.half);
       }
-    // (8 requests of 7 rows behind 128K: 39 us for 44 with the bytes kept in the caches)
-    if (live == u.q * P.s.G) Kind<D, DT, PREFIX>::template part<kPrefix, true>(P, u, row, p0, p1, memory.prefix);
+    // (8 requests of 7 rows behind 128K: 39 us for 44 with the bytes kept in the caches; of several tiles none passes them: 32
+    // requests of 8 rows at d 256 behind 30K 31.7 us for 32.5 with the first one past them, drafts of int8 51.2 for 52.1, 64 of 4
+    // at d 128 behind 8K 30.0 for 30.2)
+    if (u.q * P.s.G <= PREFIX) Kind<D, DT, PREFIX>::template part<kPrefix, true>(P, u, row, p0, p1, memory.prefix);
     else Kind<D, DT, PREFIX>::template part<kPrefix, false>(P, u, row, p0, p1, memory.prefix);
   } else {
     u.kv = last;
