@@ -566,8 +566,11 @@ UGBS_API int ugbs_cache_attend(const ugbs_cache* c, const void* Q, const void* c
 UGBS_API size_t ugbs_cache_workspace_bytes(const ugbs_cache* c);
 
 /* Attention of a batch whose requests list common first pages (a system prompt, several
- * answers to one prompt): each common page is read once for all rows of a group instead of
- * once for each request.  The result is that of ugbs_cache_attend but for the order of sums.
+ * answers to one prompt): each common page is read once for a tile of rows of all requests of
+ * a group instead of once for each request: 64 rows of a kv head (32 at d 256; 16 where the batch has no more).
+ * The result is that of ugbs_cache_attend but for the order of sums and, with e4m3, d 128 or 256 and more than 16 query rows
+ * of the batch to a kv head, for the first product of common pages, which may take queries as two e4m3 numbers
+ * there, as ugbs_cache_attend does from 33 (17 at d 256) rows of a request on.
  *
  * ugbs_cache_share lays a step out, once for all its layers, after ugbs_cache_plan:
  *   group   : [B] int32: requests of equal numbers >= 0 are a group; negative: alone.  What a
@@ -585,8 +588,6 @@ UGBS_API int ugbs_cache_share(const ugbs_cache* c, const int32_t* group, const i
  *   table, kv_lens, q_lens, share : those of the ugbs_cache_share call, which comes before on the stream,
  *             with a c of the same batch, heads, head_dim, max_pages and rows.
  *   workspace : at least ugbs_cache_shared_workspace_bytes(c) bytes, else as for ugbs_cache_attend.
- *   For common pages the rows of all requests count together, batch rows H / H_kv, where
- *   ugbs_cache_attend takes a query channel as two e4m3 numbers.
  *   Where rows H / H_kv > 128 (pieces of prompts), each request's rows fill tiles of their own,
  *   bound by the matrix cores; there, with one request and with batch rows H > 2^20 nothing is
  *   shared and the call is ugbs_cache_attend. */
@@ -609,7 +610,8 @@ UGBS_API size_t ugbs_cache_shared_workspace_bytes(const ugbs_cache* c);
  *   (y_a, y_b) -> rot_gain (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = position freqs[j],
  * a, b = j, j + rot_dim / 2 (UGBS_HALVES) or 2 j, 2 j + 1 (UGBS_NEIGHBOURS).  Values stay
  * as they are.  In fp32, angles in 64 bits (t is off by at most 2^-51 |t| + 2^-23), rounded to bf16
- * once. */
+ * once.  Squares are fp32 too: a head whose sum of squares passes its range becomes 0, a mean with norm_eps below
+ * 2^-126 may count as 0. */
 typedef enum { UGBS_HALVES = 0, UGBS_NEIGHBOURS = 1 } ugbs_pairs;
 
 typedef struct ugbs_heads {
@@ -636,7 +638,7 @@ typedef struct ugbs_rows {
 /* Rows to queries, keys and values by heads.
  *   q, k, v   : H, H_kv and H_kv heads.
  *   q_norm, k_norm : [d] fp32, 16-byte aligned, the norms' weights; either may be NULL (no norm).
- *   freqs     : [rot_dim / 2] fp64, 8-byte aligned, angle per position of each pair (may
+ *   freqs     : [rot_dim / 2] fp64, 8-byte aligned, finite, angle per position of each pair (may
  *               be NULL with rot_dim 0).
  *   positions : [axes, B, rows] int32 or NULL: token i of request b then is at position
  *               first[b] + i on every axis.

@@ -136,7 +136,8 @@ __device__ __forceinline__ int splits_of(const Lengths& r, int per) { return r.p
 // tiles that read the same pages (kv head, part) on one XCD, one after another, so
 // that its L2 serves all but the first: workgroup j runs on XCD j mod 8, so groups
 // are dealt out 8 at a time, those that are left over in turn (4 of them keep to two XCDs each; in a
-// row they run on all 8: drafts of d 256 behind 5 prompts, 14 draws, 58.7 us, in turn 57.5).  Uniform over the wave.
+// row they run on all 8: drafts of d 256 behind 5 prompts, 14 draws, 58.7 us, in turn 57.5; 25 kinds of pieces of prompts in
+// a row 1.4% less to 3.6% more, 42 of 1014 tokens of 28/4 heads 320 us, in turn 316).  Uniform over the wave.
 enum Order { kParts, kGroups, kJoinTiles, kLongTilesOnly };
 template <Order ORDER>
 __device__ __forceinline__ void locate(const CacheAttendParams& P, int at, int tiles, int slots_before, Part* out) {

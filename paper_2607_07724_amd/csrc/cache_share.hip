@@ -5,13 +5,14 @@
 // maximum, the sum and the weighted values of each, the result is
 //   (2^(M_P - M) o_P + 2^(M_R - M) o_R) / (2^(M_P - M) l_P + 2^(M_R - M) l_R),  M = max(M_P, M_R),
 // the join that parts along the pages need anyway.  What is won is bytes: a page of the prefix
-// is read once for up to 64 rows of a kv head, of all requests of the group, instead of once for each request.
+// is read once for a tile of rows of a kv head, of all requests of the group, instead of once for each request: 64 rows
+// (32 at d 256; 16 where the batch has no more).
 //
 // ugbs_cache_share finds, once a step, what the requests of a group have in common (their table
 // rows are compared, so nothing but the table says what is shared) and lays the parts out,
 // as ugbs_cache_attend does for itself; the launches of a layer only look their part up.
 // What bounds it: a long prefix with many rows the matrix cores and the vector ALU (32 requests of 28/4 heads, d 128, behind
-// 128K tokens: 84 to 88 us, 325 with every request alone, 44 at the rate of a large product); less of it the parts'
+// 128K tokens: 81 to 88 us, 325 with every request alone, 44 at the rate of a large product); less of it the parts'
 // starts and ends and the join (64 requests of 32/8 heads behind 8K tokens: 30 us, of which the join 5; 75 alone).
 #include <algorithm>
 
@@ -168,8 +169,8 @@ constexpr int kTimes = 8;                 // candidates for the longest part's t
 constexpr float kLonger = 0.1f;           // so much longer than the one before
 
 // The parts, PER requests a thread.  PER 1: every workgroup forms the requests' entries and sums for itself, in LDS, and
-// writes its share.  More: one workgroup, which finds its entries again in the plan.  FIND: what share_compare_kernel does
-// comes first here, for few requests of few pages.
+// writes its share (1000 requests, with the comparison: 15 us).  More: one workgroup, which finds its entries again in the plan
+// (2000: 47, 4000: 80).  FIND: what share_compare_kernel does comes first here, for few requests of few pages.
 template <int THREADS, int PER, bool FIND>
 __global__ void __launch_bounds__(THREADS) share_plan_kernel(CacheAttendParams P, const int32_t* __restrict__ group, int own_rows,
                                                              int prefix_rows, int parts) {
@@ -497,8 +498,8 @@ __device__ __forceinline__ void shared_part(const CacheAttendParams& P) {
         return tiles_part<D, DT, 2, 2, kWaves, false, kPrefix>(P, u, row, p0, p1, memory.half);
       }
     // (8 requests of 7 rows behind 128K: 39 us for 44 with the bytes kept in the caches; of several tiles none passes them: 32
-    // requests of 8 rows at d 256 behind 30K 31.7 us for 32.5 with the first one past them, drafts of int8 51.2 for 52.1, 64 of 4
-    // at d 128 behind 8K 30.0 for 30.2)
+    // requests of 8 rows at d 256 behind 30K 32.1 us for 32.8 with the first one past them, 40 of 32 in 5 groups 43.3 for 46.2, in
+    // int8 57 either way, 64 of 4 at d 128 behind 8K 29.9 for 30.1)
     if (u.q * P.s.G <= PREFIX) Kind<D, DT, PREFIX>::template part<kPrefix, true>(P, u, row, p0, p1, memory.prefix);
     else Kind<D, DT, PREFIX>::template part<kPrefix, false>(P, u, row, p0, p1, memory.prefix);
   } else {

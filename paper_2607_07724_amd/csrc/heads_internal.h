@@ -4,8 +4,9 @@
 // A row is the d channels of one head of one token.  d / 16 lanes hold it, 16 channels
 // each, as two eights, 8 l .. 8 l + 7 and as many half the rotated channels further on; the other
 // channels' likewise.  So the lanes' first eights follow each other, as do their second ones (a
-// store of every other 16 bytes costs: 15000 tokens of 16/2 heads, d 256, 66 us for 57), and a lane
-// rotates by itself, whichever way channels are paired, with 8 angles.
+// store of every other 16 bytes costs: 15000 tokens of 16/2 heads, d 256, 66 us for 57; runs that are no
+// whole lines, as those of rot 64, still 2 of these), and a lane rotates by itself, whichever way channels
+// are paired, with 8 angles.
 //   y = x / sqrt(mean x^2 + eps) * w,   (y_a, y_b) -> (y_a cos t - y_b sin t, y_b cos t + y_a sin t)
 // in fp32, rounded to bf16 once at the end.  Products and sums are written as the
 // operations they are (no contraction left to the compiler), so that every kernel that
