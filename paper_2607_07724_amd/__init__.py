@@ -785,7 +785,7 @@ class CacheStep:
         torch = _get_torch()
         B, dev = self.table.shape[0], self.table.device
         if not (torch.is_tensor(requests) and requests.is_cuda):
-            requests = torch.arange(B)[requests].to(dev)
+            requests = torch.arange(B)[requests,].to(dev)
         if requests.dtype == torch.bool:
             return requests
         x = requests.reshape(-1).long()

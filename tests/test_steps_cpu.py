@@ -1,4 +1,5 @@
 """The host's side of steps over the cache, without a GPU: forks, requests that leave pages, steps that are refused."""
+import numpy as np
 import pytest
 import torch
 
@@ -54,7 +55,7 @@ def test_requests_with_tokens_of_their_own_are_not_forked():
     assert [step.table[b].tolist() for b in (0, 1, 3)] == [row(b, 5) for b in (0, 1, 3)]
 
 
-@pytest.mark.parametrize("requests", [2, [2], [2, 2], [-4], torch.tensor([2, 2]), torch.arange(B) == 2, slice(2, 3)])
+@pytest.mark.parametrize("requests", [2, [2], (2,), (2, 2), range(2, 3), np.array([2]), [2, 2], [-4], torch.tensor([2, 2]), torch.arange(B) == 2, slice(2, 3)])
 def test_requests_are_named_as_torch_takes_them(requests):
     step = made([200, 0, 0, 0, 0, 0])
     step.fork(0, requests, 64)
